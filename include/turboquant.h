@@ -487,6 +487,127 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
                     int64_t row_step, void* stream);
 
 /*
+ * ---- A cache of keys and values in pages, 8 bits a value ----
+ *
+ * Beside the codes above (1 to 4 bits, one length for all groups) a serving program keeps some caches in 8 bits: many
+ * sequences of different lengths, in pages of some tokens each that lie anywhere in a pool.  One page of one head is a
+ * block [page_tokens][d] of codes with one scale; a code c stands for c * scale.
+ *   Codes   TQ_PAGE_E4M3: OCP e4m3 (torch.float8_e4m3fn);  TQ_PAGE_I8: int8 in [-127, 127].
+ *   Scales  tq_pages_append makes powers of two: the smallest 2^e with amax / 2^e <= 448 (127), e in [-40, 40], amax over
+ *           the block's finite values; larger values (infinities among them) take the largest code, NaN takes NaN (int8: 0).
+ *           A power of two lets a block whose scale grows be coded again without a second rounding of what stays
+ *           representable.  tq_pages_attend takes any positive scales.
+ *   Bounds  (optional) the smallest and largest value of every channel of a page's keys, rounded outward to bf16.
+ *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
+ *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
+ *   lens[s] tokens of sequence s, the call's own new tokens among them: row j of its count rows is at position
+ *           lens[s] - count + j.  Rows at positions below zero are no tokens (nothing stored, output zero).
+ */
+typedef enum { TQ_PAGE_E4M3 = 0, TQ_PAGE_I8 = 1 } tq_page_type;
+
+typedef struct tq_pages {
+  int32_t d;            /* 64, 128 or 256, else TQ_ERR_UNSUPPORTED                                          */
+  int32_t n_heads;      /* heads of keys and values                                                         */
+  int32_t page_tokens;  /* 16, 32, 64 or 128, else TQ_ERR_UNSUPPORTED                                       */
+  int32_t type;         /* tq_page_type                                                                     */
+  int64_t n_pages;      /* n_pages * n_heads * page_tokens at most 2^34, n_pages at most 2^31 - 1           */
+  void* k;              /* device [n_pages][n_heads][page_tokens][d] codes, 16-byte aligned                 */
+  void* v;
+  float* k_scale;       /* device [n_pages][n_heads]                                                        */
+  float* v_scale;
+  uint16_t* bounds;     /* device [n_pages][n_heads][2][d] bf16 (lower, upper), 16-byte aligned, or NULL    */
+  int32_t* refs;        /* device [n_pages]: sequences that hold the page, 0 = free; for the pool calls     */
+  void* workspace;      /* device scratch, 16-byte aligned; calls that share one must not overlap in time
+                           (two streams, or two captured graphs that may run at once: two workspaces)      */
+  size_t workspace_bytes;
+} tq_pages;
+
+typedef struct tq_batch {
+  int32_t n_seqs;
+  int32_t max_new;        /* at least the largest count of rows of a sequence; further rows are left alone  */
+  int64_t n_rows;         /* rows of the k / v / q / out arrays; rows outside [0, n_rows) are left alone    */
+  int32_t width;          /* table entries of a sequence: tokens behind width * page_tokens are not there   */
+  int64_t table_stride;   /* elements between the rows of the table, at least width                         */
+  int32_t* table;         /* device [n_seqs][table_stride]                                                  */
+  int32_t* lens;          /* device [n_seqs]                                                                */
+  const int32_t* starts;  /* device [n_seqs + 1]: the rows of sequence s are [starts[s], starts[s + 1]).
+                             NULL: every sequence has max_new rows, [s * max_new, (s + 1) * max_new)        */
+} tq_batch;
+
+/*
+ * Store the new keys and values.  k, v: device, n_rows rows (dtype TQ_F32 or TQ_BF16) of n_heads vectors, `ld_row` elements
+ * between rows and `ld_head` between heads; 16-byte aligned, strides multiples of 16 bytes, else TQ_ERR_UNSUPPORTED.
+ * A page whose first token is among the new ones starts afresh; in any other the scale grows to max(old, new) and the codes
+ * that were there are rounded to it.  Slots behind the last token stay as they were.  Two sequences of one call must not
+ * store into the same page.  No workspace.
+ */
+tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, const void* v, int32_t dtype, int64_t ld_row,
+                          int64_t ld_head, void* stream);
+
+/*
+ * Attention over the pages: the row at position p of a sequence sees the tokens j <= p, and of these only j > p - window
+ * where window > 0.  Query head i of n_heads_q (a multiple of n_heads) reads head i / (n_heads_q / n_heads):
+ *   out = sum_j softmax_j(scale <q, k_j>) v_j,   lse = ln sum_j exp(scale <q, k_j>).
+ * A row that sees nothing has out = 0 and lse = -inf.  A value that a row does not see never reaches it, whatever it is;
+ * a NaN among the values it sees makes its output NaN in that coordinate, or in all.
+ *   q, out   device, n_rows rows (both TQ_F32 or both TQ_BF16) of n_heads_q vectors, strides in elements; 16-byte
+ *            aligned, strides multiples of 16 bytes, else TQ_ERR_UNSUPPORTED.
+ *   lse      device [n_rows][n_heads_q] fp32, or NULL.
+ *   chosen   NULL: all tokens.  Else device [n_rows][n_heads][n_chosen]: places in the sequence's table (page i holds
+ *            tokens [i * page_tokens, ..)) that the row's query heads read, in any order; entries outside [0, width) are
+ *            skipped, one that is there twice counts twice.
+ * Sums, maxima and weights are fp32.  Codes are exact factors in 16 bits; a bf16 query is one exact factor, an fp32 one
+ * three; a softmax weight is taken in fp16 (bf16 output: relative error 2^-11, below the output's own half step 2^-8) or as
+ * two fp16 pieces (fp32 output: 2^-22), no closer than 2^-32 of the row's largest weight times value scale.
+ * Uses c->workspace: tq_pages_attend_workspace_bytes() bytes (0 where no sequence is cut into ranges), which depend on
+ * b's sizes and not on its device arrays.
+ */
+size_t tq_pages_attend_workspace_bytes(const tq_pages* c, const tq_batch* b, int32_t n_heads_q, int32_t n_chosen, int32_t window);
+tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, int32_t dtype, int64_t ldq_row,
+                          int64_t ldq_head, int32_t n_heads_q, float scale, int32_t window, const int32_t* chosen,
+                          int32_t n_chosen, void* out, int64_t ldo_row, int64_t ldo_head, float* lse, void* stream);
+
+/*
+ * Choose pages for tq_pages_attend by their bounds.  For the row at position p and a head of the cache, page i (i up to
+ * p / page_tokens) has the score
+ *   max over the head's query heads of  sum_j max(q_j lower_ij, q_j upper_ij),
+ * which no <q, k> of its keys exceeds; the sum is taken in 64 bits and rounded to fp32 once.  The first keep_first and the
+ * last keep_last pages come first, then the others by score, equal scores by lower i, NaN last.  An entry of the table that
+ * is no page is never chosen.
+ *   chosen   device out [n_rows][n_heads][n_chosen]: the chosen pages' places in the table, ascending, then -1.
+ * q as above.  n_chosen in [1, 1024], keep_first + keep_last <= n_chosen.  width <= 65536.  Uses c->workspace.
+ */
+size_t tq_pages_select_workspace_bytes(const tq_pages* c, const tq_batch* b);
+tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, int32_t dtype, int64_t ldq_row,
+                          int64_t ldq_head, int32_t n_heads_q, int32_t keep_first, int32_t keep_last, int32_t* chosen,
+                          int32_t n_chosen, void* stream);
+
+/*
+ * The pool.  c->refs counts the table rows that hold a page; 0 is a free page.  Free pages are given out lowest first, in
+ * the order of the rows (entries of the list); `missing` (device, nullable) is set to the number of pages that were wanted
+ * and not there (their entries stay -1).  Results do not depend on any order of execution.  n_pages <= 2^22 for these calls.
+ *   tq_pages_reserve  every entry that is no page among those that hold the last max_new positions below lens[s] gets a
+ *                     free page (refs = 1): to be called before an append, with lens already counting the new tokens.
+ *   tq_pages_fork     row children[i] (which holds no pages) becomes a copy of row parents[i]: full pages are shared
+ *                     (refs + 1), a last page that is not full is copied into a free one.  Children are distinct rows and
+ *                     no parents; a row outside [0, n_seqs) is skipped.
+ *   tq_pages_free     rows rows[i] give back what they hold (refs - 1): their entries become -1, their lens 0.
+ *   tq_pages_compact  the pages in use move to [0, n_live): those at n_live and above, in order, into the free pages below,
+ *                     in order.  Contents, refs and the batch's table follow; n_live: device, nullable.  Every table row
+ *                     that holds pages must be in the batch.
+ *   tq_pages_copy     page src[i] -> page dst[i] (device arrays of n pairs): codes, scales, bounds; not refs.  A page
+ *                     that is copied to is in no other pair; a pair with a page outside [0, n_pages) is skipped.
+ * Reserve, fork and compact use c->workspace: tq_pages_pool_workspace_bytes() (n: entries of a fork's lists, else 0).
+ */
+size_t tq_pages_pool_workspace_bytes(const tq_pages* c, int64_t n);
+tq_status tq_pages_reserve(const tq_pages* c, const tq_batch* b, int32_t* missing, void* stream);
+tq_status tq_pages_fork(const tq_pages* c, const tq_batch* b, const int32_t* parents, const int32_t* children, int32_t n,
+                        int32_t* missing, void* stream);
+tq_status tq_pages_free(const tq_pages* c, const tq_batch* b, const int32_t* rows, int32_t n, void* stream);
+tq_status tq_pages_compact(const tq_pages* c, const tq_batch* b, int32_t* n_live, void* stream);
+tq_status tq_pages_copy(const tq_pages* c, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
+
+/*
  * Codec stages on their own (HBM-bound; they are also what the bit-exactness
  * tests drive): the decision idx_j = argmin_k |y_j - c_k| of Alg. 1 plus
  * packing for given rotated coordinates y[n][d]; the sign packing of Alg. 2

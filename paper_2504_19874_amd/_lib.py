@@ -34,7 +34,38 @@ class TqParams(C.Structure):
 TQ_FLAG_FP32_MFMA, TQ_FLAG_DEQUANT_IMAGES, TQ_FLAG_SIGN_IMAGES = 1, 2, 4
 
 
-_P = C.POINTER(TqParams)
+class TqPages(C.Structure):
+    _fields_ = [
+        ("d", C.c_int32),
+        ("n_heads", C.c_int32),
+        ("page_tokens", C.c_int32),
+        ("type", C.c_int32),
+        ("n_pages", C.c_int64),
+        ("k", C.c_void_p),
+        ("v", C.c_void_p),
+        ("k_scale", C.c_void_p),
+        ("v_scale", C.c_void_p),
+        ("bounds", C.c_void_p),
+        ("refs", C.c_void_p),
+        ("workspace", C.c_void_p),
+        ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class TqBatch(C.Structure):
+    _fields_ = [
+        ("n_seqs", C.c_int32),
+        ("max_new", C.c_int32),
+        ("n_rows", C.c_int64),
+        ("width", C.c_int32),
+        ("table_stride", C.c_int64),
+        ("table", C.c_void_p),
+        ("lens", C.c_void_p),
+        ("starts", C.c_void_p),
+    ]
+
+
+_P, _PG, _B = C.POINTER(TqParams), C.POINTER(TqPages), C.POINTER(TqBatch)
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 
 # name -> (restype, argtypes); mirrors include/turboquant.h
@@ -68,6 +99,17 @@ SIGNATURES = {
     "tq_attend_cache": (C.c_int, [_P, _P, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64,
                                   C.c_float, _vp, _i64, _vp]),
     "tq_append": (C.c_int, [_P, _vp, C.c_int, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _vp]),
+    "tq_pages_append": (C.c_int, [_PG, _B, _vp, _vp, _i32, _i64, _i64, _vp]),
+    "tq_pages_attend_workspace_bytes": (C.c_size_t, [_PG, _B, _i32, _i32, _i32]),
+    "tq_pages_attend": (C.c_int, [_PG, _B, _vp, _i32, _i64, _i64, _i32, C.c_float, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _vp]),
+    "tq_pages_select_workspace_bytes": (C.c_size_t, [_PG, _B]),
+    "tq_pages_select": (C.c_int, [_PG, _B, _vp, _i32, _i64, _i64, _i32, _i32, _i32, _vp, _i32, _vp]),
+    "tq_pages_pool_workspace_bytes": (C.c_size_t, [_PG, _i64]),
+    "tq_pages_reserve": (C.c_int, [_PG, _B, _vp, _vp]),
+    "tq_pages_fork": (C.c_int, [_PG, _B, _vp, _vp, _i32, _vp, _vp]),
+    "tq_pages_free": (C.c_int, [_PG, _B, _vp, _i32, _vp]),
+    "tq_pages_compact": (C.c_int, [_PG, _B, _vp, _vp]),
+    "tq_pages_copy": (C.c_int, [_PG, _vp, _vp, _i64, _vp]),
     "tq_stage_pack": (C.c_int, [_P, _vp, _i64, _vp, _vp]),
     "tq_stage_sign_pack": (C.c_int, [_i32, _vp, _i64, _vp, _vp]),
     "tq_stage_unpack": (C.c_int, [_P, _vp, _i64, _vp, _vp]),

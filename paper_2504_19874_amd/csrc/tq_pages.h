@@ -1,0 +1,108 @@
+// Shared by the kernels of the 8-bit paged cache (tq_pages_*.hip).
+#pragma once
+#include "tq_internal.h"
+
+namespace tq {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kPageE4m3 = TQ_PAGE_E4M3, kPageI8 = TQ_PAGE_I8;
+constexpr int kPageScaleLow = -40, kPageScaleHigh = 40;  // exponents of the scales that append makes
+
+// A call's cache and batch as the kernels take them (tq_pages, tq_batch).
+struct PagesView {
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  uint16_t* bounds;
+  int32_t* refs;
+  int n_pages, heads, log2_page;
+};
+struct BatchView {
+  int32_t *table, *lens;
+  const int32_t* starts;
+  int64_t table_stride, n_rows;
+  int width, n_seqs, max_new;
+  // first row of sequence s, and its rows (no more than max_new of them are worked on)
+  __device__ __forceinline__ int64_t first_row(int s) const { return starts != nullptr ? starts[s] : (int64_t)s * max_new; }
+  __device__ __forceinline__ int count(int s) const { return starts != nullptr ? starts[s + 1] - starts[s] : max_new; }
+};
+
+// Rows of keys, values, queries or outputs.
+struct PagesRows {
+  const void* p;
+  int64_t ld_row, ld_head;
+};
+
+// codes of one dword as fp32
+template <int CT>
+__device__ __forceinline__ void page_decode(uint32_t w, float (&x)[4]) {
+  if constexpr (CT == kPageE4m3) {
+    const float2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  }
+}
+// four values over their scale as codes: to nearest, ties to even, the largest code beyond it; NaN stays NaN in e4m3 and is 0 in int8
+template <int CT>
+__device__ __forceinline__ uint32_t page_encode(const float (&x)[4]) {
+  constexpr float top = CT == kPageE4m3 ? 448.f : 127.f;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = fminf(fmaxf(x[i], -top), top);
+    if (x[i] != x[i]) y[i] = CT == kPageE4m3 ? x[i] : 0.f;
+  }
+  if constexpr (CT == kPageE4m3) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+  } else {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * i);
+    return w;
+  }
+}
+
+struct PagesAttendArgs {
+  PagesView c;
+  BatchView b;
+  PagesRows q, out;
+  float* lse;
+  const int32_t* chosen;
+  int n_chosen;
+  int group;  // query heads that read a head of the cache
+  float scale;
+  int window;  // of tokens that a row sees; INT_MAX: all
+};
+hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
+
+hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,
+                               hipStream_t s);
+
+struct PagesSelectArgs {
+  PagesView c;
+  BatchView b;
+  PagesRows q;
+  int group, keep_first, keep_last, n_chosen;
+  int32_t* chosen;
+  float* scores;  // [n_rows][heads][width]
+};
+hipError_t launch_pages_select(int d, bool f32, const PagesSelectArgs& a, hipStream_t s);
+
+hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t* list, int32_t* missing, hipStream_t s);
+hipError_t launch_pages_fork(const PagesView& c, const BatchView& b, int d, const int32_t* parents, const int32_t* children, int n, int32_t* list,
+                             int32_t* fresh, int32_t* missing, hipStream_t s);
+hipError_t launch_pages_free(const PagesView& c, const BatchView& b, const int32_t* rows, int n, hipStream_t s);
+hipError_t launch_pages_compact(const PagesView& c, const BatchView& b, int d, int32_t* plan, int32_t* move, int32_t* at, int32_t* n_live, hipStream_t s);
+hipError_t launch_pages_copy(const PagesView& c, int d, const int32_t* src, const int32_t* dst, int64_t n, hipStream_t s);
+
+}  // namespace tq

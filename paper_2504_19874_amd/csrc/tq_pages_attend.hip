@@ -1,0 +1,400 @@
+// Attention over pages of 8-bit keys and values.
+//
+//   out = sum_j softmax_j(scale <q, k_j>) v_j,  one pass over the keys with the running maximum and sum of the softmax.
+//
+// A wavefront has 16 rows (of one sequence and head of the cache: its new tokens times the query heads that read this head) and walks
+// the keys in tiles of 32, two subtiles of 16; a subtile never leaves a page.  Products on v_mfma_f32_16x16x32:
+//   S^T = K Q^T    A = 16 keys, B = 16 rows.  The codes are exact in bf16; so is a bf16 query, an fp32 one is three bf16 pieces.
+//                  Lane (r = lane % 16, g = lane / 16) has row r of a subtile's keys, bytes [g d / 4, (g + 1) d / 4): which
+//                  coordinate is which k of the product does not matter as long as both sides agree.
+//   O^T += V^T P^T A = 16 coordinates, B = 16 rows, k = 32 keys.  S^T leaves lane (r, g) with the weights of row r and the keys
+//                  4 g + 0..3 of both subtiles, which are eight k of this product already: no weight changes its lane.  The lane
+//                  fetches the same eight keys' coordinates [r d / 16, (r + 1) d / 16) and turns them by 4 x 4 bytes in
+//                  registers.  The codes are exact in fp16; the weights are fp16 (two pieces for an fp32 output).
+// With C the base-2 logarithm, lane sums and frames are:  x = log2(e) scale s + log2(v_scale) - M + BASE,  w = 2^x,
+// O = sum w c_v,  l = sum w / v_scale; M is the largest log2(e) scale s + log2(v_scale) so far or up to HEAD below it (a new M costs
+// a pass over O, so it is taken only where a weight would leave fp16's range).  The scale of a value block sits in the exponent of
+// its weights and never costs a product.  With |log2 v_scale| <= 40 a weight that underflows (2^-149 below 2^BASE) is less than
+// 2^-60 of l.
+#include <climits>
+
+#include "tq_pages.h"
+
+namespace tq {
+
+namespace {
+
+constexpr float BASE = 7.f, HEAD = 8.f;  // weights up to 2^15 of fp16's 2^16
+constexpr float LOG2E_HI = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float swap_max(float v) {  // over the four lanes that share lane % 16
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float swap_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// eight codes as bf16 / fp16, exactly
+template <int CT>
+__device__ __forceinline__ bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
+  union {
+    bf16x2_t h[4];
+    uint32_t w[4];
+    bf16x8_t v;
+  } u;
+  if constexpr (CT == kPageE4m3) {
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, false);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, true);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, false);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, true);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
+      u.w[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w >> 8)), __float_as_uint((float)(int8_t)w), 0x07060302u);
+    }
+  }
+  return u.v;
+}
+template <int CT>
+__device__ __forceinline__ half8_t codes_fp16(uint32_t lo, uint32_t hi) {
+  union {
+    half2_t h[4];
+    half8_t v;
+  } u;
+  if constexpr (CT == kPageE4m3) {
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
+      u.h[i] = __builtin_convertvector(float2_t{(float)(int8_t)w, (float)(int8_t)(w >> 8)}, half2_t);
+    }
+  }
+  return u.v;
+}
+
+// bytes that are the NaN of e4m3, as 0xff
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
+}
+
+// a tile on its way: 32 keys and values, and what its two subtiles are
+template <int D>
+struct Tile {
+  uint32_t k[2][D / 16], v[8][D / 64];
+  int pos[2];             // of the subtile's first token (far beyond every row where its page is none)
+  float ks[2], lv[2], iv[2];  // scale of its keys, base-2 logarithm and inverse of that of its values
+};
+
+template <int D, int CT, bool F32>
+__global__ __launch_bounds__(64) void pages_attend_kernel(const PagesAttendArgs a) {
+  constexpr int KS = D / 32;  // k steps of S, and pieces of eight bytes of a lane's keys
+  constexpr int VE = D / 16;  // coordinates of a lane's values
+  constexpr int QP = F32 ? 3 : 1;
+  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
+  const int heads = a.c.heads, group = a.group, page = 1 << a.c.log2_page;
+  // the unit: a sequence and head (a row and head where the pages are chosen), and a tile of its rows
+  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * group + 15) / 16);
+  const int tile = (int)(blockIdx.x % (unsigned)row_tiles);
+  unsigned unit = blockIdx.x / (unsigned)row_tiles;
+  const int h = (int)(unit % (unsigned)heads);
+  unit /= (unsigned)heads;
+  const int s = a.chosen != nullptr ? (int)(unit / (unsigned)a.b.max_new) : (int)unit;
+  const int t0 = a.chosen != nullptr ? (int)(unit % (unsigned)a.b.max_new) : 0;  // the unit's first row of the sequence
+  const int whole = a.b.count(s), count = min(whole, a.b.max_new);
+  const int rows = (a.chosen != nullptr ? (t0 < count ? 1 : 0) : count) * group;
+  if (tile * 16 >= rows) return;
+  const int len = a.b.lens[s];
+  const int64_t row0 = a.b.first_row(s);
+
+  // this lane's row: query head and token, its position and where it lies
+  const int mine = tile * 16 + r;
+  const int t = t0 + (mine < rows ? mine : rows - 1) / group, head = h * group + (mine < rows ? mine : rows - 1) % group;
+  const int64_t row = row0 + t;
+  const bool there = mine < rows && row >= 0 && row < a.b.n_rows;
+  const int pos = len - whole + t;
+  // the tile's smallest and largest position
+  const int pos_lo = len - whole + t0 + tile * 16 / group, pos_hi = len - whole + t0 + min(tile * 16 + 15, rows - 1) / group;
+
+  bf16x8_t q[QP][KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    const int64_t at = row * a.q.ld_row + head * a.q.ld_head + g * (D / 4) + 8 * k;
+    if constexpr (F32) {
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (there) {
+        const float4_t u = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at);
+        const float4_t w = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = u[i], x[4 + i] = w[i];
+      }
+      // three pieces of eight bits: what a rounding leaves is exact in fp32 (an infinite value's pieces: itself and NaN)
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          q[p][k][i] = (__bf16)x[i];
+          x[i] -= (float)q[p][k][i];
+        }
+    } else {
+      union {
+        uint4_t w;
+        bf16x8_t v;
+      } u;
+      u.w = uint4_t{0, 0, 0, 0};
+      if (there) u.w = *reinterpret_cast<const uint4_t*>(static_cast<const uint16_t*>(a.q.p) + at);
+      q[0][k] = u.v;
+    }
+  }
+
+  // keys: [lo, hi) of the sequence, or all of the chosen pages
+  const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
+  int lo = 0, hi;
+  if (a.chosen != nullptr) {
+    hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)INT_MAX - 64);
+  } else {
+    hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 64));
+    lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
+  }
+  const int tiles = hi > lo ? (hi - lo + 31) >> 5 : 0;
+  const int32_t* const table = a.b.table + (int64_t)s * a.b.table_stride;
+  const int32_t* const list = a.chosen != nullptr ? a.chosen + ((row0 + t0) * heads + h) * a.n_chosen : nullptr;
+  const bool listed = a.chosen == nullptr || (row0 + t0 >= 0 && row0 + t0 < a.b.n_rows);
+
+  // a lane knows one subtile of the next 64
+  int sub_at = 0, sub_pos = 0;
+  float sub_ks = 1.f, sub_lv = 0.f, sub_iv = 1.f;
+  const auto look_up = [&](int first) {
+    const int64_t at = (int64_t)lo + 16 * ((int64_t)2 * first + lane);
+    sub_at = -1;
+    sub_pos = 0x70000000;
+    sub_ks = 1.f, sub_lv = 0.f, sub_iv = 1.f;
+    if (at < hi && listed) {
+      int i = (int)(at >> a.c.log2_page);
+      if (list != nullptr) i = list[i];
+      if (i >= 0 && i < a.b.width) {
+        const int p = table[i];
+        if (p >= 0 && p < a.c.n_pages) {
+          const int off = (int)at & (page - 1);
+          const int64_t block = (int64_t)p * heads + h;
+          sub_at = (int)(((block << a.c.log2_page) + off) >> 4);
+          sub_pos = (int)min(((int64_t)i << a.c.log2_page) + off, (int64_t)0x70000000);
+          sub_ks = a.c.k_scale[block];
+          const float vs = a.c.v_scale[block];
+          sub_lv = __builtin_amdgcn_logf(vs);
+          sub_iv = 1.f / vs;
+        }
+      }
+    }
+  };
+  const auto load = [&](Tile<D>& b, int i) {
+    if ((i & 31) == 0) look_up(i);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int l = ((i & 31) << 1) + u;
+      const int at = __builtin_amdgcn_readlane(sub_at, l);
+      b.pos[u] = __builtin_amdgcn_readlane(sub_pos, l);
+      b.ks[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_ks), l));
+      b.lv[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_lv), l));
+      b.iv[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_iv), l));
+      const int64_t off = (int64_t)(at < 0 ? 0 : at) * (16 * D);  // where there is no page, the pool's first bytes, unused
+      const uint8_t* const kp = a.c.k + off + r * D + g * (D / 4);
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) *reinterpret_cast<uint4_t*>(&b.k[u][4 * j]) = *reinterpret_cast<const uint4_t*>(kp + 16 * j);
+      const uint8_t* const vp = a.c.v + off + 4 * g * D + r * VE;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t* const to = b.v[4 * u + j];
+        if constexpr (D == 64) to[0] = *reinterpret_cast<const uint32_t*>(vp + j * D);
+        if constexpr (D == 128) *reinterpret_cast<uint2_t*>(to) = *reinterpret_cast<const uint2_t*>(vp + j * D);
+        if constexpr (D == 256) *reinterpret_cast<uint4_t*>(to) = *reinterpret_cast<const uint4_t*>(vp + j * D);
+      }
+    }
+  };
+
+  float4_t o[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) o[e] = float4_t{0.f, 0.f, 0.f, 0.f};
+  float l = 0.f, M = -INFINITY, shift = 0.f, limit = -3e38f;  // shift = BASE - M, limit: of x before a new M is taken
+  const double c64 = (double)a.scale * 1.4426950408889634074;
+  const float c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
+
+  const auto step = [&](Tile<D>& b) {
+    float4_t acc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      acc[u] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const bf16x8_t f = codes_bf16<CT>(b.k[u][2 * k], b.k[u][2 * k + 1]);
+#pragma unroll
+        for (int p = QP - 1; p >= 0; --p) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[p][k], acc[u], 0, 0, 0);
+      }
+    }
+    float x[8];
+    const auto exponents = [&] {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float ch = b.ks[u] * c_hi, cl = b.ks[u] * c_lo, add = b.lv[u] + shift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[4 * u + i] = fmaf(acc[u][i], ch, add);
+          if (F32) x[4 * u + i] = fmaf(acc[u][i], cl, x[4 * u + i]);
+        }
+      }
+    };
+    exponents();
+    // all rows see the whole tile, or some do not
+    const bool inner = max(b.pos[0], b.pos[1]) + 15 <= pos_lo && (int64_t)min(b.pos[0], b.pos[1]) > (int64_t)pos_hi - a.window;
+    uint32_t hidden = 0;  // bit j: key j is not seen
+    if (!inner) {
+      uint32_t poison = 0;
+      if constexpr (CT == kPageE4m3) {
+        // 0 * NaN is NaN: a NaN among the values leaves the product, and comes back by the weights of the rows that see it
+        uint32_t any = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int w = 0; w < D / 64; ++w) any |= nan_bytes(b.v[j][w]);
+        if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t here = 0;
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) {
+              const uint32_t n = nan_bytes(b.v[j][w]);
+              b.v[j][w] &= ~n;
+              here |= n;
+            }
+            const uint64_t lanes = __builtin_amdgcn_ballot_w64(here != 0);
+            poison |= ((lanes >> (16 * g)) & 0xffffu) != 0 ? 1u << j : 0u;
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = b.pos[j >> 2] + 4 * g + (j & 3);
+        const bool seen = key <= pos && (int64_t)key > (int64_t)pos - a.window;
+        hidden |= seen ? 0u : 1u << j;
+        if (seen && ((poison >> j) & 1)) acc[j >> 2][j & 3] = __builtin_nanf("");
+      }
+      exponents();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((hidden >> j) & 1) x[j] = -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+    if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+      const float reach = swap_max(top);  // in the old frame: reach = log2 .. + shift
+      const float next = fmaxf(M, reach - shift);
+      const float down = M == next || M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - next);
+      if (next != -INFINITY) {
+        M = next;
+        shift = BASE - M;
+        limit = BASE + HEAD;
+      }
+      l *= down;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) o[e] *= down;
+      exponents();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((hidden >> j) & 1) x[j] = -INFINITY;
+    }
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      w[j] = __builtin_amdgcn_exp2f(x[j]);
+      l = fmaf(w[j], b.iv[j >> 2], l);
+    }
+    half8_t p_hi, p_lo;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      p_hi[j] = (_Float16)w[j];
+      p_lo[j] = (_Float16)(w[j] - (float)p_hi[j]);
+    }
+#pragma unroll
+    for (int e4 = 0; e4 < VE / 4; ++e4) {
+      uint32_t turned[2][4];  // [subtile][coordinate]: four keys
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t w0 = b.v[4 * u][e4], w1 = b.v[4 * u + 1][e4], w2 = b.v[4 * u + 2][e4], w3 = b.v[4 * u + 3][e4];
+        const uint32_t a0 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a1 = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
+        const uint32_t b0 = __builtin_amdgcn_perm(w3, w2, 0x05010400u), b1 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+        turned[u][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+        turned[u][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+        turned[u][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+        turned[u][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const half8_t f = codes_fp16<CT>(turned[0][e], turned[1][e]);
+        float4_t& to = o[4 * e4 + e];
+        if (F32) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_lo, to, 0, 0, 0);
+        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_hi, to, 0, 0, 0);
+      }
+    }
+  };
+
+  Tile<D> buf;
+  for (int i = 0; i < tiles; ++i) {
+    load(buf, i);
+    step(buf);
+  }
+
+  // lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
+  l = swap_sum(l);
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  if (!there) return;
+  const int64_t at = row * a.out.ld_row + head * a.out.ld_head + g * (D / 4);
+#pragma unroll
+  for (int c = 0; c < D / 4; c += 8) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = o[(c + i) % VE][(c + i) / VE] * inv;
+    if constexpr (F32) {
+      float* const to = static_cast<float*>(const_cast<void*>(a.out.p)) + at + c;
+      *reinterpret_cast<float4_t*>(to) = float4_t{y[0], y[1], y[2], y[3]};
+      *reinterpret_cast<float4_t*>(to + 4) = float4_t{y[4], y[5], y[6], y[7]};
+    } else {
+      bf16x8_t z;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = (__bf16)y[i];
+      *reinterpret_cast<bf16x8_t*>(static_cast<uint16_t*>(const_cast<void*>(a.out.p)) + at + c) = z;
+    }
+  }
+  if (a.lse != nullptr && g == 0) a.lse[row * heads * group + head] = l != 0.f ? (__builtin_amdgcn_logf(l) - shift) * LN2 : -INFINITY;
+}
+
+template <int D, int CT>
+hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
+  const int64_t units = (int64_t)a.b.n_seqs * a.c.heads * (a.chosen != nullptr ? a.b.max_new : 1);
+  const int64_t row_tiles = ((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 15) / 16;
+  const dim3 grid((unsigned)(units * row_tiles));
+  if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64), 0, s, a);
+  else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s) {
+  const bool i8 = type == kPageI8;
+  if (d == 64) return i8 ? launch<64, kPageI8>(f32, a, s) : launch<64, kPageE4m3>(f32, a, s);
+  if (d == 128) return i8 ? launch<128, kPageI8>(f32, a, s) : launch<128, kPageE4m3>(f32, a, s);
+  return i8 ? launch<256, kPageI8>(f32, a, s) : launch<256, kPageE4m3>(f32, a, s);
+}
+
+}  // namespace tq

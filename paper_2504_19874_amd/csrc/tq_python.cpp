@@ -10,6 +10,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -236,9 +237,215 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// --- the paged cache: p.c (a tq_pages struct) and p.k, whose GPU every tensor is on and which is the current one ------------
+
+struct Cache {
+  const tq_pages* c;
+  c10::Device device;
+};
+Cache cache(PyObject* const* o) {
+  Py_buffer b;
+  if (PyObject_GetBuffer(o[0], &b, PyBUF_SIMPLE) != 0) {
+    PyErr_Clear();
+    throw NotPlain{};
+  }
+  const bool whole = (size_t)b.len == sizeof(tq_pages);
+  const tq_pages* c = static_cast<const tq_pages*>(b.buf);
+  PyBuffer_Release(&b);
+  const at::Tensor* k = tensor(o[1]);
+  if (!whole || k == nullptr || k->device().index() != c10::hip::current_device()) throw NotPlain{};
+  return Cache{c, k->device()};
+}
+
+const at::Tensor& there(const Cache& p, PyObject* o, c10::ScalarType type, int64_t dims) {
+  const at::Tensor* t = tensor(o);
+  if (t == nullptr || t->scalar_type() != type || t->dim() != dims || t->device() != p.device) throw NotPlain{};
+  return *t;
+}
+
+int32_t* ints(const Cache& p, PyObject* o, int64_t n) {
+  const at::Tensor& t = there(p, o, at::kInt, 1);
+  if (t.size(0) != n || !t.is_contiguous()) throw NotPlain{};
+  return static_cast<int32_t*>(t.data_ptr());
+}
+
+// table, lens, starts (or None): a batch of n_rows rows
+tq_batch batch(const Cache& p, int64_t n_rows, PyObject* table, PyObject* lens, PyObject* starts, int32_t max_new) {
+  const at::Tensor& t = there(p, table, at::kInt, 2);
+  const int64_t n = t.size(0), width = t.size(1);
+  if (n > INT32_MAX || width > INT32_MAX || max_new < 0 || (width > 1 && t.stride(1) != 1) || (n > 1 && t.stride(0) < width)) throw NotPlain{};
+  if (starts == Py_None && n_rows < n * max_new) throw NotPlain{};
+  tq_batch b;
+  b.n_seqs = (int32_t)n, b.max_new = max_new, b.n_rows = n_rows, b.width = (int32_t)width;
+  b.table_stride = n > 1 ? t.stride(0) : width;
+  b.table = static_cast<int32_t*>(t.data_ptr());
+  b.lens = lens == Py_None ? nullptr : ints(p, lens, n);
+  b.starts = starts == Py_None ? nullptr : ints(p, starts, n + 1);
+  return b;
+}
+
+struct Vectors {
+  void* ptr;
+  int64_t rows, heads, ld_row, ld_head;
+  int32_t dtype;
+};
+Vectors vectors(const Cache& p, PyObject* o) {
+  const at::Tensor* t = tensor(o);
+  if (t == nullptr || t->dim() != 3 || t->size(2) != p.c->d || t->stride(2) != 1 || t->device() != p.device) throw NotPlain{};
+  Vectors v;
+  v.ptr = t->data_ptr(), v.rows = t->size(0), v.heads = t->size(1);
+  v.ld_row = v.rows > 1 ? t->stride(0) : 0, v.ld_head = v.heads > 1 ? t->stride(1) : 0;
+  if (v.heads > INT32_MAX) throw NotPlain{};
+  if (t->scalar_type() == at::kFloat) v.dtype = TQ_F32;
+  else if (t->scalar_type() == at::kBFloat16) v.dtype = TQ_BF16;
+  else throw NotPlain{};
+  return v;
+}
+
+void* stream_of(const Cache& p) { return static_cast<void*>(c10::hip::getCurrentHIPStream(p.device.index()).stream()); }
+
+// p.c, p.k, k, v, table, lens, starts, max_new
+PyObject* pages_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&] {
+    const Cache p = cache(a);
+    const Vectors k = vectors(p, a[2]), v = vectors(p, a[3]);
+    if (k.rows != v.rows || k.heads != v.heads || k.heads != p.c->n_heads || k.dtype != v.dtype || k.ld_row != v.ld_row || k.ld_head != v.ld_head)
+      throw NotPlain{};
+    const tq_batch b = batch(p, k.rows, a[4], a[5], a[6], integer32(a[7]));
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_append(p.c, &b, k.ptr, v.ptr, k.dtype, k.ld_row, k.ld_head, s); });
+  });
+}
+
+// [rows][heads of the cache][n] places of pages, or None
+int32_t* places(const Cache& p, PyObject* o, int64_t rows, int32_t* n) {
+  *n = 0;
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = there(p, o, at::kInt, 3);
+  if (t.size(0) != rows || t.size(1) != p.c->n_heads || t.size(2) < 1 || t.size(2) > INT32_MAX || !t.is_contiguous()) throw NotPlain{};
+  *n = (int32_t)t.size(2);
+  return static_cast<int32_t*>(t.data_ptr());
+}
+
+// p.c, p.k, q, table, lens, starts, max_new, scale, out, lse, window, chosen
+PyObject* pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 12, [&] {
+    const Cache p = cache(a);
+    const Vectors q = vectors(p, a[2]), out = vectors(p, a[8]);
+    if (q.rows != out.rows || q.heads != out.heads || q.dtype != out.dtype || q.heads < 1 || q.heads % p.c->n_heads != 0 || q.rows < 1 ||
+        (out.rows > 1 && out.ld_row == 0) || (out.heads > 1 && out.ld_head == 0) || !PyFloat_CheckExact(a[7]))
+      throw NotPlain{};
+    const float scale = (float)PyFloat_AS_DOUBLE(a[7]);
+    float* lse = nullptr;
+    if (a[9] != Py_None) {
+      const at::Tensor& t = there(p, a[9], at::kFloat, 2);
+      if (t.size(0) != q.rows || t.size(1) != q.heads || !t.is_contiguous()) throw NotPlain{};
+      lse = static_cast<float*>(t.data_ptr());
+    }
+    const int32_t window = integer32(a[10]);
+    int32_t n_chosen;
+    const int32_t* const chosen = places(p, a[11], q.rows, &n_chosen);
+    const tq_batch b = batch(p, q.rows, a[3], a[4], a[5], integer32(a[6]));
+    if (p.c->workspace_bytes < tq_pages_attend_workspace_bytes(p.c, &b, (int32_t)q.heads, n_chosen, window)) throw NotPlain{};
+    void* const s = stream_of(p);
+    return unlocked([&] {
+      return tq_pages_attend(p.c, &b, q.ptr, q.dtype, q.ld_row, q.ld_head, (int32_t)q.heads, scale, window, chosen, n_chosen, out.ptr, out.ld_row,
+                             out.ld_head, lse, s);
+    });
+  });
+}
+
+// p.c, p.k, q, table, lens, starts, max_new, chosen, keep_first, keep_last
+PyObject* pages_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 10, [&] {
+    const Cache p = cache(a);
+    const Vectors q = vectors(p, a[2]);
+    if (q.heads < 1 || q.heads % p.c->n_heads != 0 || q.rows < 1 || a[7] == Py_None || p.c->bounds == nullptr) throw NotPlain{};
+    int32_t n_chosen;
+    int32_t* const chosen = places(p, a[7], q.rows, &n_chosen);
+    const tq_batch b = batch(p, q.rows, a[3], a[4], a[5], integer32(a[6]));
+    if (p.c->workspace_bytes < tq_pages_select_workspace_bytes(p.c, &b)) throw NotPlain{};
+    const int32_t first = integer32(a[8]), last = integer32(a[9]);
+    void* const s = stream_of(p);
+    return unlocked([&] {
+      return tq_pages_select(p.c, &b, q.ptr, q.dtype, q.ld_row, q.ld_head, (int32_t)q.heads, first, last, chosen, n_chosen, s);
+    });
+  });
+}
+
+void pool(const Cache& p, int64_t n) {
+  if (p.c->refs == nullptr || p.c->workspace_bytes < tq_pages_pool_workspace_bytes(p.c, n)) throw NotPlain{};
+}
+int32_t* one(const Cache& p, PyObject* o) { return o == Py_None ? nullptr : ints(p, o, 1); }
+
+// p.c, p.k, table, lens, max_new, missing
+PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 6, [&] {
+    const Cache p = cache(a);
+    pool(p, 0);
+    const tq_batch b = batch(p, INT32_MAX, a[2], a[3], Py_None, integer32(a[4]));
+    int32_t* const missing = one(p, a[5]);
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_reserve(p.c, &b, missing, s); });
+  });
+}
+
+// p.c, p.k, table, lens, parents, children, missing
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 7, [&] {
+    const Cache p = cache(a);
+    const int64_t forks = there(p, a[4], at::kInt, 1).size(0);
+    if (forks > INT32_MAX) throw NotPlain{};
+    pool(p, forks);
+    const int32_t *const parents = ints(p, a[4], forks), *const children = ints(p, a[5], forks);
+    const tq_batch b = batch(p, 0, a[2], a[3], Py_None, 0);
+    int32_t* const missing = one(p, a[6]);
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_fork(p.c, &b, parents, children, (int32_t)forks, missing, s); });
+  });
+}
+
+// p.c, p.k, table, lens, rows
+PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 5, [&] {
+    const Cache p = cache(a);
+    const int64_t many = there(p, a[4], at::kInt, 1).size(0);
+    if (many > INT32_MAX || p.c->refs == nullptr) throw NotPlain{};
+    const int32_t* const rows = ints(p, a[4], many);
+    const tq_batch b = batch(p, 0, a[2], a[3], Py_None, 0);
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_free(p.c, &b, rows, (int32_t)many, s); });
+  });
+}
+
+// p.c, p.k, table, n_live
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 4, [&] {
+    const Cache p = cache(a);
+    pool(p, 0);
+    const tq_batch b = batch(p, 0, a[2], Py_None, Py_None, 0);
+    int32_t* const live = one(p, a[3]);
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_compact(p.c, &b, live, s); });
+  });
+}
+
+// p.c, p.k, src, dst
+PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 4, [&] {
+    const Cache p = cache(a);
+    const int64_t pairs = there(p, a[2], at::kInt, 1).size(0);
+    const int32_t *const src = ints(p, a[2], pairs), *const dst = ints(p, a[3], pairs);
+    void* const s = stream_of(p);
+    return unlocked([&] { return tq_pages_copy(p.c, src, dst, pairs, s); });
+  });
+}
+
 #define TQ_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TQ_METHOD(quantize_mse), TQ_METHOD(quantize_prod), TQ_METHOD(append), TQ_METHOD(dequantize),
-                         TQ_METHOD(score), TQ_METHOD(attend), {nullptr, nullptr, 0, nullptr}};
+                         TQ_METHOD(score), TQ_METHOD(attend), TQ_METHOD(pages_append), TQ_METHOD(pages_attend),
+                         TQ_METHOD(pages_select), TQ_METHOD(pages_reserve), TQ_METHOD(pages_fork), TQ_METHOD(pages_free),
+                         TQ_METHOD(pages_compact), TQ_METHOD(pages_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
