@@ -82,7 +82,13 @@ struct PagesAttendArgs {
   int group;  // query heads that read a head of the cache
   float scale;
   int window;  // of tokens that a row sees; INT_MAX: all
+  int splits;   // ranges that the keys of a unit are cut into
+  float* part;  // what they leave, [n_rows][query heads][splits][4 + d]; with one range unused
 };
+// workgroups of one range each: sequences (or rows) times heads times tiles of query rows
+int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen);
+int pages_attend_splits(const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
+size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits);
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
 
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,

@@ -77,6 +77,19 @@ bool launchable(int64_t a, int64_t b, int64_t c) {
   return a <= most && b <= most && a * b <= most && c <= most && a * b * c <= most;
 }
 
+// the grids of attend: ranges of keys at most 64
+bool attend_fits(const tq_batch* b, int heads, int group, bool chosen) {
+  const int64_t rows = (chosen ? 1 : (int64_t)b->max_new) * group;
+  return rows <= INT_MAX - 16 && launchable((int64_t)b->n_seqs * (chosen ? b->max_new : 1), heads, (rows + 15) / 16) &&
+         launchable((int64_t)b->n_seqs * b->max_new, (int64_t)heads * group, 1);
+}
+size_t attend_part_bytes(const tq_pages* c, const tq_batch* b, int group, bool chosen, int n_chosen, int window, int* splits) {
+  const BatchView v = view(b);
+  const int n = pages_attend_splits(v, c->n_heads, group, chosen, n_chosen, log2_of(c->page_tokens), window > 0 ? window : INT_MAX);
+  if (splits != nullptr) *splits = n;
+  return pages_attend_part_bytes(c->d, v, c->n_heads, group, n);
+}
+
 size_t pool_bytes(const tq_pages* c, int64_t n) { return (size_t)(3 * c->n_pages + n + 64) * sizeof(int32_t); }
 
 tq_status check_pool(const tq_pages* c, const tq_batch* b, int64_t n) {
@@ -119,7 +132,9 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
 }
 
 size_t tq_pages_attend_workspace_bytes(const tq_pages* c, const tq_batch* b, int32_t n_heads_q, int32_t n_chosen, int32_t window) {
-  return 0;
+  if (check_queries(c, b, n_heads_q) != TQ_OK || n_chosen < 0 || window < 0) return 0;
+  if (!attend_fits(b, c->n_heads, n_heads_q / c->n_heads, n_chosen > 0)) return 0;
+  return attend_part_bytes(c, b, n_heads_q / c->n_heads, n_chosen > 0, n_chosen, window, nullptr);
 }
 
 tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, int32_t dtype, int64_t ldq_row, int64_t ldq_head, int32_t n_heads_q,
@@ -141,8 +156,10 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
   a.q = PagesRows{q, ldq_row, ldq_head}, a.out = PagesRows{out, ldo_row, ldo_head};
   a.lse = lse, a.chosen = chosen, a.n_chosen = n_chosen, a.group = n_heads_q / c->n_heads;
   a.scale = scale, a.window = window > 0 ? window : INT_MAX;
-  const int64_t rows = (chosen != nullptr ? 1 : (int64_t)b->max_new) * a.group;
-  if (rows > INT_MAX - 16 || !launchable((int64_t)b->n_seqs * (chosen != nullptr ? b->max_new : 1), c->n_heads, (rows + 15) / 16)) return TQ_ERR_UNSUPPORTED;
+  if (!attend_fits(b, c->n_heads, a.group, chosen != nullptr)) return TQ_ERR_UNSUPPORTED;
+  const size_t need = attend_part_bytes(c, b, a.group, chosen != nullptr, n_chosen, window, &a.splits);
+  if (need > 0 && (c->workspace == nullptr || c->workspace_bytes < need || misaligned(c->workspace))) return TQ_ERR_WORKSPACE;
+  a.part = static_cast<float*>(c->workspace);
   return from_hip(launch_pages_attend(c->d, c->type, dtype == TQ_F32, a, static_cast<hipStream_t>(stream)));
 }
 

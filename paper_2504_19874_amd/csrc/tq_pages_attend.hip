@@ -54,6 +54,7 @@ __device__ __forceinline__ bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
     u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, false);
     u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, true);
   } else {
+    asm("" : "+v"(lo), "+v"(hi));  // (whole words: else the compiler carries a tile through the loop a byte a register)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
@@ -74,6 +75,7 @@ __device__ __forceinline__ half8_t codes_fp16(uint32_t lo, uint32_t hi) {
     u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false);
     u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
   } else {
+    asm("" : "+v"(lo), "+v"(hi));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
@@ -82,6 +84,33 @@ __device__ __forceinline__ half8_t codes_fp16(uint32_t lo, uint32_t hi) {
   }
   return u.v;
 }
+
+// coordinates [first, first + N) of an output row: the sums over the weights' sum
+template <int N, bool F32>
+__device__ __forceinline__ void store_row(const PagesRows& out, int64_t row, int head, int first, const float (&y)[N], float sum) {
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
+  const int64_t at = row * out.ld_row + head * out.ld_head + first;
+  if constexpr (F32) {
+    typedef float vec __attribute__((ext_vector_type(N < 4 ? N : 4)));
+#pragma unroll
+    for (int c = 0; c < N; c += 4) {
+      vec z;
+#pragma unroll
+      for (int i = 0; i < (N < 4 ? N : 4); ++i) z[i] = y[c + i] * inv;
+      *reinterpret_cast<vec*>(static_cast<float*>(const_cast<void*>(out.p)) + at + c) = z;
+    }
+  } else {
+    typedef __bf16 vec __attribute__((ext_vector_type(N < 8 ? N : 8)));
+#pragma unroll
+    for (int c = 0; c < N; c += 8) {
+      vec z;
+#pragma unroll
+      for (int i = 0; i < (N < 8 ? N : 8); ++i) z[i] = (__bf16)(y[c + i] * inv);
+      *reinterpret_cast<vec*>(static_cast<uint16_t*>(const_cast<void*>(out.p)) + at + c) = z;
+    }
+  }
+}
+__device__ __forceinline__ float log_sum(float M, float sum) { return sum != 0.f ? (__builtin_amdgcn_logf(sum) + (M - BASE)) * LN2 : -INFINITY; }
 
 // bytes that are the NaN of e4m3, as 0xff
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
@@ -96,17 +125,27 @@ struct Tile {
   float ks[2], lv[2], iv[2];  // scale of its keys, base-2 logarithm and inverse of that of its values
 };
 
+constexpr int WAVES = 4;  // of a workgroup: each has a part of its keys
+
+// What a range of keys leaves for pages_join_kernel: [0] M, [1] l, [4, 4 + D) O.
+template <int D>
+constexpr int kPart = 4 + D;
+
 template <int D, int CT, bool F32>
-__global__ __launch_bounds__(64) void pages_attend_kernel(const PagesAttendArgs a) {
+__global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAttendArgs a) {
+  __shared__ float o_s[2][16][D + 4];
+  __shared__ float ml_s[WAVES][16][2];
   constexpr int KS = D / 32;  // k steps of S, and pieces of eight bytes of a lane's keys
   constexpr int VE = D / 16;  // coordinates of a lane's values
   constexpr int QP = F32 ? 3 : 1;
-  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int heads = a.c.heads, group = a.group, page = 1 << a.c.log2_page;
   // the unit: a sequence and head (a row and head where the pages are chosen), and a tile of its rows
   const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * group + 15) / 16);
-  const int tile = (int)(blockIdx.x % (unsigned)row_tiles);
-  unsigned unit = blockIdx.x / (unsigned)row_tiles;
+  const int split = (int)(blockIdx.x % (unsigned)a.splits);
+  unsigned unit = blockIdx.x / (unsigned)a.splits;
+  const int tile = (int)(unit % (unsigned)row_tiles);
+  unit /= (unsigned)row_tiles;
   const int h = (int)(unit % (unsigned)heads);
   unit /= (unsigned)heads;
   const int s = a.chosen != nullptr ? (int)(unit / (unsigned)a.b.max_new) : (int)unit;
@@ -167,6 +206,9 @@ __global__ __launch_bounds__(64) void pages_attend_kernel(const PagesAttendArgs 
     lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
   }
   const int tiles = hi > lo ? (hi - lo + 31) >> 5 : 0;
+  // this wavefront's: an equal part of them, in one piece
+  const int each = (tiles + a.splits * WAVES - 1) / (a.splits * WAVES);
+  const int begin = (split * WAVES + wave) * each, end = min(begin + each, tiles);
   const int32_t* const table = a.b.table + (int64_t)s * a.b.table_stride;
   const int32_t* const list = a.chosen != nullptr ? a.chosen + ((row0 + t0) * heads + h) * a.n_chosen : nullptr;
   const bool listed = a.chosen == nullptr || (row0 + t0 >= 0 && row0 + t0 < a.b.n_rows);
@@ -198,10 +240,10 @@ __global__ __launch_bounds__(64) void pages_attend_kernel(const PagesAttendArgs 
     }
   };
   const auto load = [&](Tile<D>& b, int i) {
-    if ((i & 31) == 0) look_up(i);
+    if (((i - begin) & 31) == 0) look_up(i);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int l = ((i & 31) << 1) + u;
+      const int l = (((i - begin) & 31) << 1) + u;
       const int at = __builtin_amdgcn_readlane(sub_at, l);
       b.pos[u] = __builtin_amdgcn_readlane(sub_pos, l);
       b.ks[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_ks), l));
@@ -348,47 +390,145 @@ __global__ __launch_bounds__(64) void pages_attend_kernel(const PagesAttendArgs 
     }
   };
 
-  Tile<D> buf;
-  for (int i = 0; i < tiles; ++i) {
-    load(buf, i);
-    step(buf);
-  }
-
-  // lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
-  l = swap_sum(l);
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  if (!there) return;
-  const int64_t at = row * a.out.ld_row + head * a.out.ld_head + g * (D / 4);
-#pragma unroll
-  for (int c = 0; c < D / 4; c += 8) {
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = o[(c + i) % VE][(c + i) / VE] * inv;
-    if constexpr (F32) {
-      float* const to = static_cast<float*>(const_cast<void*>(a.out.p)) + at + c;
-      *reinterpret_cast<float4_t*>(to) = float4_t{y[0], y[1], y[2], y[3]};
-      *reinterpret_cast<float4_t*>(to + 4) = float4_t{y[4], y[5], y[6], y[7]};
-    } else {
-      bf16x8_t z;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = (__bf16)y[i];
-      *reinterpret_cast<bf16x8_t*>(static_cast<uint16_t*>(const_cast<void*>(a.out.p)) + at + c) = z;
+  // the next tile is asked for before a tile's products
+  Tile<D> one, two;
+  if (begin < end) load(one, begin);
+  for (int i = begin; i < end; i += 2) {
+    if (i + 1 < end) load(two, i + 1);
+    step(one);
+    if (i + 1 < end) {
+      if (i + 2 < end) load(one, i + 2);
+      step(two);
     }
   }
-  if (a.lse != nullptr && g == 0) a.lse[row * heads * group + head] = l != 0.f ? (__builtin_amdgcn_logf(l) - shift) * LN2 : -INFINITY;
+
+  // The wavefronts' sums in one frame.  Lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
+  l = swap_sum(l);
+  if (g == 0) ml_s[wave][r][0] = M, ml_s[wave][r][1] = l;
+  __syncthreads();
+  float top = ml_s[0][r][0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml_s[w][r][0]);
+  const float down = M == -INFINITY && l == 0.f ? 0.f : M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+  float* const mine_s = &o_s[wave & 1][r][g * (D / 4)];
+  for (int w = 0; w < WAVES; w += 2) {
+    if ((wave & ~1) == w) {
+#pragma unroll
+      for (int c = 0; c < D / 4; c += 4) {
+        float4_t y = {};
+        if (w != 0) y = *reinterpret_cast<const float4_t*>(mine_s + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += o[(c + i) % VE][(c + i) / VE] * down;
+        *reinterpret_cast<float4_t*>(mine_s + c) = y;
+      }
+    }
+    __syncthreads();
+  }
+
+  // thread: one row, D / 16 coordinates of it
+  const int out_r = threadIdx.x >> 4, first = (threadIdx.x & 15) * VE;
+  const int m2 = tile * 16 + out_r;
+  if (m2 >= rows) return;
+  const int64_t row2 = row0 + t0 + m2 / group;
+  const int head2 = h * group + m2 % group;
+  if (row2 < 0 || row2 >= a.b.n_rows) return;
+  float m = ml_s[0][out_r][0], sum = 0.f;
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ml_s[w][out_r][0]);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const float mw = ml_s[w][out_r][0], lw = ml_s[w][out_r][1];
+    sum += lw == 0.f ? 0.f : mw == m ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
+  }
+  float y[VE];
+#pragma unroll
+  for (int c = 0; c < VE; c += 4) {
+    const float4_t u = *reinterpret_cast<const float4_t*>(&o_s[0][out_r][first + c]), w = *reinterpret_cast<const float4_t*>(&o_s[1][out_r][first + c]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[c + i] = u[i] + w[i];
+  }
+  if (a.splits > 1) {
+    float* const part = a.part + ((row2 * heads * group + head2) * a.splits + split) * kPart<D>;
+#pragma unroll
+    for (int c = 0; c < VE; c += 4) *reinterpret_cast<float4_t*>(part + 4 + first + c) = float4_t{y[c], y[c + 1], y[c + 2], y[c + 3]};
+    if (first == 0) part[0] = m, part[1] = sum;
+    return;
+  }
+  store_row<VE, F32>(a.out, row2, head2, first, y, sum);
+  if (a.lse != nullptr && first == 0) a.lse[row2 * heads * group + head2] = log_sum(m, sum);
+}
+
+// one wavefront for each row and head: the ranges of keys in one frame
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void pages_join_kernel(const PagesAttendArgs a) {
+  constexpr int VE = D / 64;
+  const int lane = threadIdx.x & 63, heads = a.c.heads * a.group;
+  int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int head = (int)(item % heads);
+  item /= heads;
+  const int s = (int)(item / a.b.max_new), t = (int)(item % a.b.max_new);
+  if (s >= a.b.n_seqs || t >= a.b.count(s)) return;
+  const int64_t row = a.b.first_row(s) + t;
+  if (row < 0 || row >= a.b.n_rows) return;
+  const float* const part = a.part + (row * heads + head) * a.splits * kPart<D>;
+  float m = -INFINITY, l = 0.f;
+  if (lane < a.splits) m = part[lane * kPart<D>], l = part[lane * kPart<D> + 1];
+  const float top = over_wavefront(m, [](float x, float y) { return fmaxf(x, y); });
+  const float f = l == 0.f ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+  const float sum = over_wavefront(f * l, [](float x, float y) { return x + y; });
+  float y[VE] = {};
+  for (int i0 = 0; i0 < a.splits; i0 += 16) {  // 16 loads on their way
+    float x[16][VE];
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+#pragma unroll
+      for (int c = 0; c < VE; ++c) x[u][c] = part[(i0 + u < a.splits ? i0 + u : 0) * kPart<D> + 4 + lane * VE + c];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i0 + u));  // (0 behind the last range)
+#pragma unroll
+      for (int c = 0; c < VE; ++c) y[c] = fmaf(w, x[u][c], y[c]);
+    }
+  }
+  store_row<VE, F32>(a.out, row, head, lane * VE, y, sum);
+  if (a.lse != nullptr && lane == 0) a.lse[row * heads + head] = log_sum(top, sum);
 }
 
 template <int D, int CT>
 hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
-  const int64_t units = (int64_t)a.b.n_seqs * a.c.heads * (a.chosen != nullptr ? a.b.max_new : 1);
-  const int64_t row_tiles = ((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 15) / 16;
-  const dim3 grid((unsigned)(units * row_tiles));
-  if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64), 0, s, a);
+  const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr) * a.splits));
+  if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64 * WAVES), 0, s, a);
+  else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64 * WAVES), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const dim3 join((unsigned)(((int64_t)a.b.n_seqs * a.b.max_new * a.c.heads * a.group + 3) / 4));
+  if (f32) hipLaunchKernelGGL((pages_join_kernel<D, true>), join, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((pages_join_kernel<D, false>), join, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen) {
+  const int64_t rows = (chosen ? 1 : (int64_t)b.max_new) * group;
+  return (int64_t)b.n_seqs * heads * (chosen ? b.max_new : 1) * ((rows + 15) / 16);
+}
+
+int pages_attend_splits(const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window) {
+  int64_t keys = (int64_t)(chosen ? n_chosen : b.width) << log2_page;
+  if (!chosen && window + b.max_new < keys) keys = window + b.max_new;
+  const int64_t units = pages_attend_units(b, heads, group, chosen), tiles = (keys + 31) / 32;
+  if (units == 0) return 1;
+  // a workgroup for every compute unit, no more ranges than there are tiles for their wavefronts.  One token of 8 x 4 heads after
+  // 65536, us by workgroups: 128 43.1, 256 34.1, 512 34.8; four after 64 chosen pages: 16.8, 14.9, 15.2; 64 tokens after up to 8192 each
+  // 125 with 512 or 1024
+  const int64_t target = device_cu_count(), fill = (target + units - 1) / units, most = (tiles + WAVES - 1) / WAVES;
+  const int64_t splits = fill < most ? fill : most;
+  return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+}
+size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits) {
+  return splits > 1 ? (size_t)b.n_rows * heads * group * splits * (4 + d) * sizeof(float) : 0;
+}
 
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s) {
   const bool i8 = type == kPageI8;
