@@ -83,13 +83,20 @@ struct PagesAttendArgs {
   float scale;
   int window;  // of tokens that a row sees; INT_MAX: all
   int splits;   // ranges that the keys of a unit are cut into
+  bool prompt;  // the kernel for prompts
   float* part;  // what they leave, [n_rows][query heads][splits][4 + d]; with one range unused
 };
 // workgroups of one range each: sequences (or rows) times heads times tiles of query rows
 int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen);
-int pages_attend_splits(const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
+struct PagesAttendPlan {
+  bool prompt;
+  int splits;
+};
+PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits);
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
+// many rows of bf16 queries, d = 64 or 128 (tq_pages_attend_prompt.hip)
+hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s);
 
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,
                                hipStream_t s);

@@ -83,11 +83,11 @@ bool attend_fits(const tq_batch* b, int heads, int group, bool chosen) {
   return rows <= INT_MAX - 16 && launchable((int64_t)b->n_seqs * (chosen ? b->max_new : 1), heads, (rows + 15) / 16) &&
          launchable((int64_t)b->n_seqs * b->max_new, (int64_t)heads * group, 1);
 }
-size_t attend_part_bytes(const tq_pages* c, const tq_batch* b, int group, bool chosen, int n_chosen, int window, int* splits) {
+size_t attend_part_bytes(const tq_pages* c, const tq_batch* b, bool f32, int group, bool chosen, int n_chosen, int window, PagesAttendPlan* plan) {
   const BatchView v = view(b);
-  const int n = pages_attend_splits(v, c->n_heads, group, chosen, n_chosen, log2_of(c->page_tokens), window > 0 ? window : INT_MAX);
-  if (splits != nullptr) *splits = n;
-  return pages_attend_part_bytes(c->d, v, c->n_heads, group, n);
+  const PagesAttendPlan n = pages_attend_plan(c->d, f32, v, c->n_heads, group, chosen, n_chosen, log2_of(c->page_tokens), window > 0 ? window : INT_MAX);
+  if (plan != nullptr) *plan = n;
+  return pages_attend_part_bytes(c->d, v, c->n_heads, group, n.splits);
 }
 
 size_t pool_bytes(const tq_pages* c, int64_t n) { return (size_t)(3 * c->n_pages + n + 64) * sizeof(int32_t); }
@@ -134,7 +134,10 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
 size_t tq_pages_attend_workspace_bytes(const tq_pages* c, const tq_batch* b, int32_t n_heads_q, int32_t n_chosen, int32_t window) {
   if (check_queries(c, b, n_heads_q) != TQ_OK || n_chosen < 0 || window < 0) return 0;
   if (!attend_fits(b, c->n_heads, n_heads_q / c->n_heads, n_chosen > 0)) return 0;
-  return attend_part_bytes(c, b, n_heads_q / c->n_heads, n_chosen > 0, n_chosen, window, nullptr);
+  const int group = n_heads_q / c->n_heads;
+  const size_t f32 = attend_part_bytes(c, b, true, group, n_chosen > 0, n_chosen, window, nullptr);
+  const size_t bf16 = attend_part_bytes(c, b, false, group, n_chosen > 0, n_chosen, window, nullptr);
+  return f32 > bf16 ? f32 : bf16;
 }
 
 tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, int32_t dtype, int64_t ldq_row, int64_t ldq_head, int32_t n_heads_q,
@@ -157,7 +160,9 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
   a.lse = lse, a.chosen = chosen, a.n_chosen = n_chosen, a.group = n_heads_q / c->n_heads;
   a.scale = scale, a.window = window > 0 ? window : INT_MAX;
   if (!attend_fits(b, c->n_heads, a.group, chosen != nullptr)) return TQ_ERR_UNSUPPORTED;
-  const size_t need = attend_part_bytes(c, b, a.group, chosen != nullptr, n_chosen, window, &a.splits);
+  PagesAttendPlan plan;
+  const size_t need = attend_part_bytes(c, b, dtype == TQ_F32, a.group, chosen != nullptr, n_chosen, window, &plan);
+  a.splits = plan.splits, a.prompt = plan.prompt;
   if (need > 0 && (c->workspace == nullptr || c->workspace_bytes < need || misaligned(c->workspace))) return TQ_ERR_WORKSPACE;
   a.part = static_cast<float*>(c->workspace);
   return from_hip(launch_pages_attend(c->d, c->type, dtype == TQ_F32, a, static_cast<hipStream_t>(stream)));

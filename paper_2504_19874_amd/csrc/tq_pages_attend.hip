@@ -16,106 +16,13 @@
 // a pass over O, so it is taken only where a weight would leave fp16's range).  The scale of a value block sits in the exponent of
 // its weights and never costs a product.  With |log2 v_scale| <= 40 a weight that underflows (2^-149 below 2^BASE) is less than
 // 2^-60 of l.
-#include <climits>
+#include <algorithm>
 
-#include "tq_pages.h"
+#include "tq_pages_attend.h"
 
 namespace tq {
 
 namespace {
-
-constexpr float BASE = 7.f, HEAD = 8.f;  // weights up to 2^15 of fp16's 2^16
-constexpr float LOG2E_HI = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ float swap_max(float v) {  // over the four lanes that share lane % 16
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float swap_sum(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-// eight codes as bf16 / fp16, exactly
-template <int CT>
-__device__ __forceinline__ bf16x8_t codes_bf16(uint32_t lo, uint32_t hi) {
-  union {
-    bf16x2_t h[4];
-    uint32_t w[4];
-    bf16x8_t v;
-  } u;
-  if constexpr (CT == kPageE4m3) {
-    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, false);
-    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, true);
-    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, false);
-    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, true);
-  } else {
-    asm("" : "+v"(lo), "+v"(hi));  // (whole words: else the compiler carries a tile through the loop a byte a register)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
-      u.w[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(w >> 8)), __float_as_uint((float)(int8_t)w), 0x07060302u);
-    }
-  }
-  return u.v;
-}
-template <int CT>
-__device__ __forceinline__ half8_t codes_fp16(uint32_t lo, uint32_t hi) {
-  union {
-    half2_t h[4];
-    half8_t v;
-  } u;
-  if constexpr (CT == kPageE4m3) {
-    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false);
-    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true);
-    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false);
-    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
-  } else {
-    asm("" : "+v"(lo), "+v"(hi));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t w = (i < 2 ? lo : hi) >> (16 * (i & 1));
-      u.h[i] = __builtin_convertvector(float2_t{(float)(int8_t)w, (float)(int8_t)(w >> 8)}, half2_t);
-    }
-  }
-  return u.v;
-}
-
-// coordinates [first, first + N) of an output row: the sums over the weights' sum
-template <int N, bool F32>
-__device__ __forceinline__ void store_row(const PagesRows& out, int64_t row, int head, int first, const float (&y)[N], float sum) {
-  const float inv = sum != 0.f ? 1.f / sum : 0.f;
-  const int64_t at = row * out.ld_row + head * out.ld_head + first;
-  if constexpr (F32) {
-    typedef float vec __attribute__((ext_vector_type(N < 4 ? N : 4)));
-#pragma unroll
-    for (int c = 0; c < N; c += 4) {
-      vec z;
-#pragma unroll
-      for (int i = 0; i < (N < 4 ? N : 4); ++i) z[i] = y[c + i] * inv;
-      *reinterpret_cast<vec*>(static_cast<float*>(const_cast<void*>(out.p)) + at + c) = z;
-    }
-  } else {
-    typedef __bf16 vec __attribute__((ext_vector_type(N < 8 ? N : 8)));
-#pragma unroll
-    for (int c = 0; c < N; c += 8) {
-      vec z;
-#pragma unroll
-      for (int i = 0; i < (N < 8 ? N : 8); ++i) z[i] = (__bf16)(y[c + i] * inv);
-      *reinterpret_cast<vec*>(static_cast<uint16_t*>(const_cast<void*>(out.p)) + at + c) = z;
-    }
-  }
-}
-__device__ __forceinline__ float log_sum(float M, float sum) { return sum != 0.f ? (__builtin_amdgcn_logf(sum) + (M - BASE)) * LN2 : -INFINITY; }
-
-// bytes that are the NaN of e4m3, as 0xff
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
-}
 
 // a tile on its way: 32 keys and values, and what its two subtiles are
 template <int D>
@@ -131,124 +38,128 @@ constexpr int WAVES = 4;  // of a workgroup: each has a part of its keys
 template <int D>
 constexpr int kPart = 4 + D;
 
-template <int D, int CT, bool F32>
-__global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAttendArgs a) {
-  __shared__ float o_s[2][16][D + 4];
-  __shared__ float ml_s[WAVES][16][2];
-  constexpr int KS = D / 32;  // k steps of S, and pieces of eight bytes of a lane's keys
-  constexpr int VE = D / 16;  // coordinates of a lane's values
-  constexpr int QP = F32 ? 3 : 1;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int heads = a.c.heads, group = a.group, page = 1 << a.c.log2_page;
-  // the unit: a sequence and head (a row and head where the pages are chosen), and a tile of its rows
-  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * group + 15) / 16);
-  const int split = (int)(blockIdx.x % (unsigned)a.splits);
-  unsigned unit = blockIdx.x / (unsigned)a.splits;
-  const int tile = (int)(unit % (unsigned)row_tiles);
-  unit /= (unsigned)row_tiles;
-  const int h = (int)(unit % (unsigned)heads);
-  unit /= (unsigned)heads;
-  const int s = a.chosen != nullptr ? (int)(unit / (unsigned)a.b.max_new) : (int)unit;
-  const int t0 = a.chosen != nullptr ? (int)(unit % (unsigned)a.b.max_new) : 0;  // the unit's first row of the sequence
-  const int whole = a.b.count(s), count = min(whole, a.b.max_new);
-  const int rows = (a.chosen != nullptr ? (t0 < count ? 1 : 0) : count) * group;
-  if (tile * 16 >= rows) return;
-  const int len = a.b.lens[s];
-  const int64_t row0 = a.b.first_row(s);
+// What a wavefront does: R tiles of 16 rows of a unit (a sequence and head; a row and head where the pages are chosen) against keys.
+template <int D, int CT, bool F32, int R>
+struct Walk {
+  static constexpr int KS = D / 32;  // k steps of S, and pieces of eight bytes of a lane's keys
+  static constexpr int VE = D / 16;  // coordinates of a lane's values
+  static constexpr int QP = F32 ? 3 : 1;
 
-  // this lane's row: query head and token, its position and where it lies
-  const int mine = tile * 16 + r;
-  const int t = t0 + (mine < rows ? mine : rows - 1) / group, head = h * group + (mine < rows ? mine : rows - 1) % group;
-  const int64_t row = row0 + t;
-  const bool there = mine < rows && row >= 0 && row < a.b.n_rows;
-  const int pos = len - whole + t;
-  // the tile's smallest and largest position
-  const int pos_lo = len - whole + t0 + tile * 16 / group, pos_hi = len - whole + t0 + min(tile * 16 + 15, rows - 1) / group;
-
-  bf16x8_t q[QP][KS];
-#pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    const int64_t at = row * a.q.ld_row + head * a.q.ld_head + g * (D / 4) + 8 * k;
-    if constexpr (F32) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (there) {
-        const float4_t u = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at);
-        const float4_t w = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = u[i], x[4 + i] = w[i];
-      }
-      // three pieces of eight bits: what a rounding leaves is exact in fp32 (an infinite value's pieces: itself and NaN)
-#pragma unroll
-      for (int p = 0; p < 3; ++p)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          q[p][k][i] = (__bf16)x[i];
-          x[i] -= (float)q[p][k][i];
-        }
-    } else {
-      union {
-        uint4_t w;
-        bf16x8_t v;
-      } u;
-      u.w = uint4_t{0, 0, 0, 0};
-      if (there) u.w = *reinterpret_cast<const uint4_t*>(static_cast<const uint16_t*>(a.q.p) + at);
-      q[0][k] = u.v;
-    }
-  }
-
-  // keys: [lo, hi) of the sequence, or all of the chosen pages
-  const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
-  int lo = 0, hi;
-  if (a.chosen != nullptr) {
-    hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)INT_MAX - 64);
-  } else {
-    hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 64));
-    lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
-  }
-  const int tiles = hi > lo ? (hi - lo + 31) >> 5 : 0;
-  // this wavefront's: an equal part of them, in one piece
-  const int each = (tiles + a.splits * WAVES - 1) / (a.splits * WAVES);
-  const int begin = (split * WAVES + wave) * each, end = min(begin + each, tiles);
-  const int32_t* const table = a.b.table + (int64_t)s * a.b.table_stride;
-  const int32_t* const list = a.chosen != nullptr ? a.chosen + ((row0 + t0) * heads + h) * a.n_chosen : nullptr;
-  const bool listed = a.chosen == nullptr || (row0 + t0 >= 0 && row0 + t0 < a.b.n_rows);
-
+  const PagesAttendArgs& a;
+  int lane, r, g, heads, h;
+  // the unit's rows; of the lane's own rows positions, and the tiles' smallest and largest
+  int rows, t0;
+  int64_t row0;
+  int pos[R], pos_lo, pos_hi;
+  // keys [lo, hi) of the sequence, or of the chosen pages put together
+  int lo, hi;
+  const int32_t *table, *list;
+  bool listed;
   // a lane knows one subtile of the next 64
-  int sub_at = 0, sub_pos = 0;
-  float sub_ks = 1.f, sub_lv = 0.f, sub_iv = 1.f;
-  const auto look_up = [&](int first) {
-    const int64_t at = (int64_t)lo + 16 * ((int64_t)2 * first + lane);
-    sub_at = -1;
-    sub_pos = 0x70000000;
-    sub_ks = 1.f, sub_lv = 0.f, sub_iv = 1.f;
-    if (at < hi && listed) {
-      int i = (int)(at >> a.c.log2_page);
-      if (list != nullptr) i = list[i];
-      if (i >= 0 && i < a.b.width) {
-        const int p = table[i];
-        if (p >= 0 && p < a.c.n_pages) {
-          const int off = (int)at & (page - 1);
-          const int64_t block = (int64_t)p * heads + h;
-          sub_at = (int)(((block << a.c.log2_page) + off) >> 4);
-          sub_pos = (int)min(((int64_t)i << a.c.log2_page) + off, (int64_t)0x70000000);
-          sub_ks = a.c.k_scale[block];
-          const float vs = a.c.v_scale[block];
-          sub_lv = __builtin_amdgcn_logf(vs);
-          sub_iv = 1.f / vs;
+  int begin;
+  Subtile sub;
+  bf16x8_t q[R][QP][KS];
+  float4_t o[R][VE];
+  float l[R], M[R], shift[R], limit[R];  // shift = BASE - M, limit: of x before a new M is taken
+  float c_hi, c_lo;
+
+  __device__ __forceinline__ explicit Walk(const PagesAttendArgs& args) : a(args) {}
+
+  __device__ __forceinline__ int64_t row_of(int m) const { return row0 + t0 + m / a.group; }
+  __device__ __forceinline__ int head_of(int m) const { return h * a.group + m % a.group; }
+
+  // the unit and its rows [first, first + 16 R); false: there are none
+  __device__ __forceinline__ bool start(unsigned unit, int first_row) {
+    lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    heads = a.c.heads;
+    h = (int)(unit % (unsigned)heads);
+    unit /= (unsigned)heads;
+    const int s = a.chosen != nullptr ? (int)(unit / (unsigned)a.b.max_new) : (int)unit;
+    t0 = a.chosen != nullptr ? (int)(unit % (unsigned)a.b.max_new) : 0;
+    const int whole = a.b.count(s), count = min(whole, a.b.max_new);
+    rows = (a.chosen != nullptr ? (t0 < count ? 1 : 0) : count) * a.group;
+    if (first_row >= rows) return false;
+    const int len = a.b.lens[s];
+    row0 = a.b.first_row(s);
+    const int at0 = len - whole + t0;
+    pos_lo = at0 + first_row / a.group, pos_hi = at0 + min(first_row + 16 * R - 1, rows - 1) / a.group;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int m = min(first_row + 16 * i + r, rows - 1);
+      const int64_t row = row_of(m);
+      const bool there = first_row + 16 * i + r < rows && row >= 0 && row < a.b.n_rows;
+      pos[i] = at0 + m / a.group;
+      load_query(i, there, row * a.q.ld_row + head_of(m) * a.q.ld_head + g * (D / 4));
+#pragma unroll
+      for (int e = 0; e < VE; ++e) o[i][e] = float4_t{0.f, 0.f, 0.f, 0.f};
+      l[i] = 0.f, M[i] = -INFINITY, shift[i] = 0.f, limit[i] = -3e38f;
+    }
+    const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
+    lo = 0;
+    if (a.chosen != nullptr) {
+      hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)INT_MAX - 64);
+    } else {
+      hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 64));
+      lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
+    }
+    table = a.b.table + (int64_t)s * a.b.table_stride;
+    list = a.chosen != nullptr ? a.chosen + ((row0 + t0) * heads + h) * a.n_chosen : nullptr;
+    listed = a.chosen == nullptr || (row0 + t0 >= 0 && row0 + t0 < a.b.n_rows);
+    const double c64 = (double)a.scale * 1.4426950408889634074;
+    c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
+    return true;
+  }
+  __device__ __forceinline__ int tiles() const { return hi > lo ? (hi - lo + 31) >> 5 : 0; }
+
+  __device__ __forceinline__ void load_query(int i, bool there, int64_t from) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int64_t at = from + 8 * k;
+      if constexpr (F32) {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (there) {
+          const float4_t u = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at);
+          const float4_t w = *reinterpret_cast<const float4_t*>(static_cast<const float*>(a.q.p) + at + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = u[e], x[4 + e] = w[e];
         }
+        // three pieces of eight bits: what a rounding leaves is exact in fp32 (an infinite value's pieces: itself and NaN)
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            q[i][p][k][e] = (__bf16)x[e];
+            x[e] -= (float)q[i][p][k][e];
+          }
+      } else {
+        union {
+          uint4_t w;
+          bf16x8_t v;
+        } u;
+        u.w = uint4_t{0, 0, 0, 0};
+        if (there) u.w = *reinterpret_cast<const uint4_t*>(static_cast<const uint16_t*>(a.q.p) + at);
+        q[i][0][k] = u.v;
       }
     }
-  };
-  const auto load = [&](Tile<D>& b, int i) {
+  }
+
+  __device__ __forceinline__ void look_up(int first) {
+    const int64_t at = (int64_t)lo + 16 * ((int64_t)2 * first + lane);
+    sub = no_subtile();
+    if (at < hi && listed) {
+      const int i = (int)(at >> a.c.log2_page);
+      sub = find_subtile(a.c, table, a.b.width, h, list != nullptr ? list[i] : i, (int)at & ((1 << a.c.log2_page) - 1));
+    }
+  }
+
+  __device__ __forceinline__ void load(Tile<D>& b, int i) {
     if (((i - begin) & 31) == 0) look_up(i);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int l = (((i - begin) & 31) << 1) + u;
-      const int at = __builtin_amdgcn_readlane(sub_at, l);
-      b.pos[u] = __builtin_amdgcn_readlane(sub_pos, l);
-      b.ks[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_ks), l));
-      b.lv[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_lv), l));
-      b.iv[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sub_iv), l));
+      const int from = (((i - begin) & 31) << 1) + u;
+      const int at = __builtin_amdgcn_readlane(sub.at, from);
+      b.pos[u] = __builtin_amdgcn_readlane(sub.pos, from);
+      b.ks[u] = lane_value(sub.ks, from), b.lv[u] = lane_value(sub.lv, from), b.iv[u] = lane_value(sub.iv, from);
       const int64_t off = (int64_t)(at < 0 ? 0 : at) * (16 * D);  // where there is no page, the pool's first bytes, unused
       const uint8_t* const kp = a.c.k + off + r * D + g * (D / 4);
 #pragma unroll
@@ -262,110 +173,104 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAtt
         if constexpr (D == 256) *reinterpret_cast<uint4_t*>(to) = *reinterpret_cast<const uint4_t*>(vp + j * D);
       }
     }
-  };
+  }
 
-  float4_t o[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) o[e] = float4_t{0.f, 0.f, 0.f, 0.f};
-  float l = 0.f, M = -INFINITY, shift = 0.f, limit = -3e38f;  // shift = BASE - M, limit: of x before a new M is taken
-  const double c64 = (double)a.scale * 1.4426950408889634074;
-  const float c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
-
-  const auto step = [&](Tile<D>& b) {
-    float4_t acc[2];
+  // x of row tile i: base-2 logarithms of its weights in the frame
+  __device__ __forceinline__ void exponents(float (&x)[8], const float4_t (&acc)[2], const Tile<D>& b, int i, uint32_t hidden) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      acc[u] = float4_t{0.f, 0.f, 0.f, 0.f};
+      const float ch = b.ks[u] * c_hi, cl = b.ks[u] * c_lo, add = b.lv[u] + shift[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[4 * u + e] = fmaf(acc[u][e], ch, add);
+        if (F32) x[4 * u + e] = fmaf(acc[u][e], cl, x[4 * u + e]);
+      }
+    }
+    if (hidden != 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((hidden >> j) & 1) x[j] = -INFINITY;
+    }
+  }
+
+  __device__ __forceinline__ void step(Tile<D>& b) {
+    float4_t acc[R][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) acc[i][u] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const bf16x8_t f = codes_bf16<CT>(b.k[u][2 * k], b.k[u][2 * k + 1]);
 #pragma unroll
-        for (int p = QP - 1; p >= 0; --p) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[p][k], acc[u], 0, 0, 0);
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[i][p][k], acc[i][u], 0, 0, 0);
       }
     }
-    float x[8];
-    const auto exponents = [&] {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const float ch = b.ks[u] * c_hi, cl = b.ks[u] * c_lo, add = b.lv[u] + shift;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[4 * u + i] = fmaf(acc[u][i], ch, add);
-          if (F32) x[4 * u + i] = fmaf(acc[u][i], cl, x[4 * u + i]);
-        }
-      }
-    };
-    exponents();
     // all rows see the whole tile, or some do not
     const bool inner = max(b.pos[0], b.pos[1]) + 15 <= pos_lo && (int64_t)min(b.pos[0], b.pos[1]) > (int64_t)pos_hi - a.window;
-    uint32_t hidden = 0;  // bit j: key j is not seen
-    if (!inner) {
-      uint32_t poison = 0;
-      if constexpr (CT == kPageE4m3) {
-        // 0 * NaN is NaN: a NaN among the values leaves the product, and comes back by the weights of the rows that see it
-        uint32_t any = 0;
+    uint32_t poison = 0;
+    if (CT == kPageE4m3 && !inner) {
+      // 0 * NaN is NaN: a NaN among the values leaves the product, and comes back by the weights of the rows that see it
+      uint32_t any = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int w = 0; w < D / 64; ++w) any |= nan_bytes(b.v[j][w]);
-        if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+        for (int w = 0; w < D / 64; ++w) any |= nan_bytes(b.v[j][w]);
+      if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint32_t here = 0;
+        for (int j = 0; j < 8; ++j) {
+          uint32_t here = 0;
 #pragma unroll
-            for (int w = 0; w < D / 64; ++w) {
-              const uint32_t n = nan_bytes(b.v[j][w]);
-              b.v[j][w] &= ~n;
-              here |= n;
-            }
-            const uint64_t lanes = __builtin_amdgcn_ballot_w64(here != 0);
-            poison |= ((lanes >> (16 * g)) & 0xffffu) != 0 ? 1u << j : 0u;
+          for (int w = 0; w < D / 64; ++w) {
+            const uint32_t n = nan_bytes(b.v[j][w]);
+            b.v[j][w] &= ~n;
+            here |= n;
           }
+          const uint64_t lanes = __builtin_amdgcn_ballot_w64(here != 0);
+          poison |= ((lanes >> (16 * g)) & 0xffffu) != 0 ? 1u << j : 0u;
         }
+      }
+    }
+    half8_t p_hi[R], p_lo[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      uint32_t hidden = 0;  // bit j: key j is not seen
+      if (!inner) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = b.pos[j >> 2] + 4 * g + (j & 3);
+          const bool seen = key <= pos[i] && (int64_t)key > (int64_t)pos[i] - a.window;
+          hidden |= seen ? 0u : 1u << j;
+          if (seen && ((poison >> j) & 1)) acc[i][j >> 2][j & 3] = __builtin_nanf("");
+        }
+      }
+      float x[8];
+      exponents(x, acc[i], b, i, hidden);
+      float top = x[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+      if (__builtin_amdgcn_ballot_w64(top > limit[i]) != 0) {
+        const float next = fmaxf(M[i], swap_max(top) - shift[i]);
+        const float down = M[i] == next || M[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M[i] - next);
+        if (next != -INFINITY) {
+          M[i] = next;
+          shift[i] = BASE - next;
+          limit[i] = BASE + HEAD;
+        }
+        l[i] *= down;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) o[i][e] *= down;
+        exponents(x, acc[i], b, i, hidden);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int key = b.pos[j >> 2] + 4 * g + (j & 3);
-        const bool seen = key <= pos && (int64_t)key > (int64_t)pos - a.window;
-        hidden |= seen ? 0u : 1u << j;
-        if (seen && ((poison >> j) & 1)) acc[j >> 2][j & 3] = __builtin_nanf("");
+        const float w = __builtin_amdgcn_exp2f(x[j]);
+        l[i] = fmaf(w, b.iv[j >> 2], l[i]);
+        p_hi[i][j] = (_Float16)w;
+        if (F32) p_lo[i][j] = (_Float16)(w - (float)p_hi[i][j]);
       }
-      exponents();
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if ((hidden >> j) & 1) x[j] = -INFINITY;
-    }
-    float top = x[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-    if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
-      const float reach = swap_max(top);  // in the old frame: reach = log2 .. + shift
-      const float next = fmaxf(M, reach - shift);
-      const float down = M == next || M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - next);
-      if (next != -INFINITY) {
-        M = next;
-        shift = BASE - M;
-        limit = BASE + HEAD;
-      }
-      l *= down;
-#pragma unroll
-      for (int e = 0; e < VE; ++e) o[e] *= down;
-      exponents();
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if ((hidden >> j) & 1) x[j] = -INFINITY;
-    }
-    float w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = __builtin_amdgcn_exp2f(x[j]);
-      l = fmaf(w[j], b.iv[j >> 2], l);
-    }
-    half8_t p_hi, p_lo;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p_hi[j] = (_Float16)w[j];
-      p_lo[j] = (_Float16)(w[j] - (float)p_hi[j]);
     }
 #pragma unroll
     for (int e4 = 0; e4 < VE / 4; ++e4) {
@@ -383,42 +288,68 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAtt
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const half8_t f = codes_fp16<CT>(turned[0][e], turned[1][e]);
-        float4_t& to = o[4 * e4 + e];
-        if (F32) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_lo, to, 0, 0, 0);
-        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_hi, to, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          float4_t& to = o[i][4 * e4 + e];
+          if (F32) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_lo[i], to, 0, 0, 0);
+          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p_hi[i], to, 0, 0, 0);
+        }
       }
-    }
-  };
-
-  // the next tile is asked for before a tile's products
-  Tile<D> one, two;
-  if (begin < end) load(one, begin);
-  for (int i = begin; i < end; i += 2) {
-    if (i + 1 < end) load(two, i + 1);
-    step(one);
-    if (i + 1 < end) {
-      if (i + 2 < end) load(one, i + 2);
-      step(two);
     }
   }
 
+  // tiles [from, to); the next tile is asked for before a tile's products
+  __device__ __forceinline__ void run(int from, int to) {
+    begin = from;
+    Tile<D> one, two;
+    if (from < to) load(one, from);
+    for (int i = from; i < to; i += 2) {
+      if (i + 1 < to) load(two, i + 1);
+      step(one);
+      if (i + 1 < to) {
+        if (i + 2 < to) load(one, i + 2);
+        step(two);
+      }
+    }
+  }
+};
+
+// One unit and 16 rows to a workgroup, whose wavefronts share the keys of one range.
+template <int D, int CT, bool F32>
+__global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAttendArgs a) {
+  constexpr int VE = D / 16;
+  __shared__ float o_s[2][16][D + 4];
+  __shared__ float ml_s[WAVES][16][2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 15) / 16);
+  const int split = (int)(blockIdx.x % (unsigned)a.splits);
+  const unsigned unit = blockIdx.x / (unsigned)a.splits;
+  const int tile = (int)(unit % (unsigned)row_tiles);
+  Walk<D, CT, F32, 1> w(a);
+  if (!w.start(unit / (unsigned)row_tiles, 16 * tile)) return;
+  // this wavefront's tiles: an equal part of them, in one piece
+  const int tiles = w.tiles(), each = (tiles + a.splits * WAVES - 1) / (a.splits * WAVES);
+  const int begin = (split * WAVES + wave) * each;
+  w.run(begin, min(begin + each, tiles));
+  const int r = w.r, g = w.g, heads = w.heads, group = a.group;
+  const float M = w.M[0], l = swap_sum(w.l[0]);
+
   // The wavefronts' sums in one frame.  Lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
-  l = swap_sum(l);
   if (g == 0) ml_s[wave][r][0] = M, ml_s[wave][r][1] = l;
   __syncthreads();
   float top = ml_s[0][r][0];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml_s[w][r][0]);
+  for (int i = 1; i < WAVES; ++i) top = fmaxf(top, ml_s[i][r][0]);
   const float down = M == -INFINITY && l == 0.f ? 0.f : M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
   float* const mine_s = &o_s[wave & 1][r][g * (D / 4)];
-  for (int w = 0; w < WAVES; w += 2) {
-    if ((wave & ~1) == w) {
+  for (int pair = 0; pair < WAVES; pair += 2) {
+    if ((wave & ~1) == pair) {
 #pragma unroll
       for (int c = 0; c < D / 4; c += 4) {
         float4_t y = {};
-        if (w != 0) y = *reinterpret_cast<const float4_t*>(mine_s + c);
+        if (pair != 0) y = *reinterpret_cast<const float4_t*>(mine_s + c);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += o[(c + i) % VE][(c + i) / VE] * down;
+        for (int i = 0; i < 4; ++i) y[i] += w.o[0][(c + i) % VE][(c + i) / VE] * down;
         *reinterpret_cast<float4_t*>(mine_s + c) = y;
       }
     }
@@ -428,24 +359,24 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAtt
   // thread: one row, D / 16 coordinates of it
   const int out_r = threadIdx.x >> 4, first = (threadIdx.x & 15) * VE;
   const int m2 = tile * 16 + out_r;
-  if (m2 >= rows) return;
-  const int64_t row2 = row0 + t0 + m2 / group;
-  const int head2 = h * group + m2 % group;
+  if (m2 >= w.rows) return;
+  const int64_t row2 = w.row_of(m2);
+  const int head2 = w.head_of(m2);
   if (row2 < 0 || row2 >= a.b.n_rows) return;
   float m = ml_s[0][out_r][0], sum = 0.f;
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ml_s[w][out_r][0]);
+  for (int i = 1; i < WAVES; ++i) m = fmaxf(m, ml_s[i][out_r][0]);
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float mw = ml_s[w][out_r][0], lw = ml_s[w][out_r][1];
+  for (int i = 0; i < WAVES; ++i) {
+    const float mw = ml_s[i][out_r][0], lw = ml_s[i][out_r][1];
     sum += lw == 0.f ? 0.f : mw == m ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
   }
   float y[VE];
 #pragma unroll
   for (int c = 0; c < VE; c += 4) {
-    const float4_t u = *reinterpret_cast<const float4_t*>(&o_s[0][out_r][first + c]), w = *reinterpret_cast<const float4_t*>(&o_s[1][out_r][first + c]);
+    const float4_t u = *reinterpret_cast<const float4_t*>(&o_s[0][out_r][first + c]), v = *reinterpret_cast<const float4_t*>(&o_s[1][out_r][first + c]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[c + i] = u[i] + w[i];
+    for (int i = 0; i < 4; ++i) y[c + i] = u[i] + v[i];
   }
   if (a.splits > 1) {
     float* const part = a.part + ((row2 * heads * group + head2) * a.splits + split) * kPart<D>;
@@ -496,10 +427,15 @@ __global__ __launch_bounds__(256) void pages_join_kernel(const PagesAttendArgs a
 
 template <int D, int CT>
 hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr) * a.splits));
-  if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64 * WAVES), 0, s, a);
-  else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64 * WAVES), 0, s, a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (a.prompt) {
+    e = launch_pages_attend_prompt(D, CT, a, s);
+  } else {
+    const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr) * a.splits));
+    if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64 * WAVES), 0, s, a);
+    else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64 * WAVES), 0, s, a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || a.splits == 1) return e;
   const dim3 join((unsigned)(((int64_t)a.b.n_seqs * a.b.max_new * a.c.heads * a.group + 3) / 4));
   if (f32) hipLaunchKernelGGL((pages_join_kernel<D, true>), join, dim3(256), 0, s, a);
@@ -514,17 +450,28 @@ int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen
   return (int64_t)b.n_seqs * heads * (chosen ? b.max_new : 1) * ((rows + 15) / 16);
 }
 
-int pages_attend_splits(const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window) {
+PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window) {
   int64_t keys = (int64_t)(chosen ? n_chosen : b.width) << log2_page;
   if (!chosen && window + b.max_new < keys) keys = window + b.max_new;
-  const int64_t units = pages_attend_units(b, heads, group, chosen), tiles = (keys + 31) / 32;
-  if (units == 0) return 1;
+  const int64_t units = pages_attend_units(b, heads, group, chosen), rows = (int64_t)b.max_new * group;
+  PagesAttendPlan plan = {false, 1};
+  if (units == 0) return plan;
+  // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys until every compute unit has a workgroup.
+  // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 991 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
+  // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 155, 16 (64 rows) 263 / 292, 32 279 / 577
+  const int64_t blocks = (int64_t)b.n_seqs * heads * ((rows + 255) / 256);
+  if (!chosen && !f32 && d != 256 && rows > 64) {
+    const int64_t fill = (device_cu_count() + blocks - 1) / blocks, most = (keys + 1023) / 1024;
+    plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)16);
+    plan.prompt = 2 * blocks * plan.splits >= device_cu_count();
+    if (plan.prompt) return plan;
+  }
   // a workgroup for every compute unit, no more ranges than there are tiles for their wavefronts.  One token of 8 x 4 heads after
   // 65536, us by workgroups: 128 43.1, 256 34.1, 512 34.8; four after 64 chosen pages: 16.8, 14.9, 15.2; 64 tokens after up to 8192 each
   // 125 with 512 or 1024
-  const int64_t target = device_cu_count(), fill = (target + units - 1) / units, most = (tiles + WAVES - 1) / WAVES;
-  const int64_t splits = fill < most ? fill : most;
-  return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+  const int64_t fill = (device_cu_count() + units - 1) / units, most = (keys + 32 * WAVES - 1) / (32 * WAVES);
+  plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)64);
+  return plan;
 }
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits) {
   return splits > 1 ? (size_t)b.n_rows * heads * group * splits * (4 + d) * sizeof(float) : 0;

@@ -173,6 +173,56 @@ def test_attend(case):
     run_attend(1, d, page, kind, dtype, heads, group, lens, new, window)
 
 
+PROMPTS = [  # more than 64 rows to a head, half the compute units with a workgroup: the kernel for prompts
+    (128, 64, "e4m3", 8, 1, [70 + 13 * i for i in range(16)], [70 - i for i in range(16)], 0),
+    (128, 16, "int8", 8, 1, [90 + 13 * i for i in range(16)], [65] * 16, 30),
+    (64, 16, "e4m3", 4, 3, [257] * 32, [26 - i % 3 for i in range(32)], 0),
+    (64, 32, "int8", 16, 2, [33 + i for i in range(8)], [33] * 8, 7),
+    (128, 128, "int8", 4, 16, [129] * 2 + [300], [129, 65, 67], 0),
+    (128, 64, "e4m3", 8, 1, [4100, 66, 3000, 1], [66, 66, 1, 1], 0),  # keys in ranges
+    (64, 64, "e4m3", 8, 1, [4100, 66, 3000, 0], [66, 66, 66, 0], 2500),
+]
+
+
+@pytest.mark.parametrize("case", PROMPTS)
+def test_prompts(case):
+    d, page, kind, heads, group, lens, new, window = case
+    run_attend(8, d, page, kind, "bf16", heads, group, lens, new, window)
+
+
+@pytest.mark.parametrize("d,dtype,seqs,new", [(128, "bf16", 1, 7), (64, "f32", 1, 20), (128, "bf16", 20, 70), (64, "bf16", 20, 70)])
+def test_what_a_row_does_not_see_does_not_reach_it(d, dtype, seqs, new):
+    """NaN among later tokens' keys and values, in what a window has left behind, and behind the last token: rows that see none of it have
+    the same bits as without it.  A NaN key makes a row NaN; a NaN value its coordinate, or the row."""
+    rng = np.random.default_rng([41, d, seqs])
+    page, heads, window = 16, 8, 40
+    b = Batch(rng, [100] * seqs, [new] * seqs, page)
+    p = filled(rng, b, heads, d, "e4m3")
+    q = torch.from_numpy(rng.standard_normal((b.rows, heads, d)).astype(np.float32)).to(DEV, TYPES[dtype])
+
+    def run():
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+        tq.tq_pages_attend(p, q, *b.args(), 0.1, out, lse=lse, window=window)
+        return out.view(seqs, new, heads, d).float(), lse.view(seqs, new, heads)
+
+    clean, clean_lse = run()
+    at = {"k": 97, "v": 95, "old": 100 - new - window}  # the last position is 99, the first row's 100 - new
+    for s in range(seqs):
+        p.k.view(torch.uint8)[b.table[s][at["k"] // page], :, at["k"] % page, 5] = 0x7f
+        p.v.view(torch.uint8)[b.table[s][at["v"] // page], :, at["v"] % page, 7] = 0xff
+        if at["old"] >= 0:
+            p.v.view(torch.uint8)[b.table[s][at["old"] // page], :, at["old"] % page] = 0x7f
+    got, got_lse = run()
+    pos = torch.arange(100 - new, 100, device=DEV)
+    sees_v = (pos >= at["v"]) & (pos - window < at["v"])
+    sees_k = (pos >= at["k"]) & (pos - window < at["k"])
+    if at["old"] >= 0:
+        assert not ((pos >= at["old"]) & (pos - window < at["old"])).any()
+    assert torch.equal(got[:, ~(sees_v | sees_k)], clean[:, ~(sees_v | sees_k)]) and torch.equal(got_lse[:, ~(sees_v | sees_k)], clean_lse[:, ~(sees_v | sees_k)])
+    assert got[:, sees_k].isnan().all() and got_lse[:, sees_k].isnan().all()
+    assert got[:, sees_v][..., 7].isnan().all() and sees_v.any() and sees_k.any()
+
+
 @pytest.mark.parametrize("d,page,kind,dtype,group,lens,new,n", [
     (128, 64, "e4m3", "bf16", 4, [700, 90], [1, 1], 5), (64, 16, "int8", "f32", 3, [300, 33], [4, 2], 9),
     (256, 32, "e4m3", "f32", 20, [200], [2], 1), (128, 16, "int8", "bf16", 16, [999], [3], 40)])
