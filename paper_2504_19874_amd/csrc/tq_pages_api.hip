@@ -185,7 +185,7 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
   if (misaligned(c->bounds)) return TQ_ERR_UNSUPPORTED;
   st = check_rows(q, dtype, ldq_row, ldq_head, c->d);
   if (st != TQ_OK) return st;
-  if (!launchable((int64_t)b->n_seqs * b->max_new, c->n_heads, (b->width + 255) / 256)) return TQ_ERR_UNSUPPORTED;
+  if (!launchable((int64_t)b->n_seqs * b->max_new, c->n_heads, (b->width + 63) / 64)) return TQ_ERR_UNSUPPORTED;
   const size_t need = tq_pages_select_workspace_bytes(c, b);
   if (need > 0 && (c->workspace == nullptr || c->workspace_bytes < need || misaligned(c->workspace))) return TQ_ERR_WORKSPACE;
   PagesSelectArgs a;

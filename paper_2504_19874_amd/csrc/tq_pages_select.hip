@@ -5,26 +5,60 @@
 // once: which page is chosen does not depend on the order of a sum.
 //
 // pages_score_kernel writes one word for every page that a row may choose, ordered like its rank: 0 no page, 1 NaN, then the
-// scores' bits in an order of unsigned numbers, all ones for pages that are kept.  pages_pick_kernel finds the n_chosen-th
-// largest word byte by byte (counts of the words that share the bytes found so far) and writes the places of what is above it, and
-// of as many equal ones as there is room for, lowest first.
+// scores' bits in an order of unsigned numbers, all ones for pages that are kept.  Sixteen lanes share a page (a lane has d / 16
+// channels of both bounds) and add up by halves: of 16 sums (4 pages of a lane group x 4 query heads) every lane ends with one.
+// Bound by memory for a few query heads: 8192 pages of 8 heads of d = 128, 33.6 MB.  A thread to a page instead read 512 bytes apart.
+// pages_pick_kernel finds the n_chosen-th largest word by its leading bits (counts of up to 256 values of the next eight, from the first
+// bit on in which the words differ) and writes the places of what is above it, and of as many equal ones as there is room for,
+// lowest first.
 #include "tq_pages.h"
 
 namespace tq {
 
 namespace {
 
-constexpr int HEADS_AT_ONCE = 4;
-
 __device__ __forceinline__ float load_value(const void* p, int64_t at, bool f32) {
   return f32 ? static_cast<const float*>(p)[at] : __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16);
 }
 
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs a, const int blocks) {
-  __shared__ double q_s[HEADS_AT_ONCE][D];
-  const int heads = a.c.heads;
-  const int place = (int)(blockIdx.x % (unsigned)blocks) * 256 + threadIdx.x;
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int XOR1 = 0xB1, XOR2 = 0x4E, HALF_MIRROR = 0x141, ROR8 = 0x128;
+
+// N sums over 16 lanes, one step: the lane whose bit S is set keeps the upper half of the sums, its partner (CTRL, in which bit S is
+// the other) the lower half; a single sum is added in both
+template <int S, int CTRL, int N, int V>
+__device__ __forceinline__ void add_halves(double (&v)[V]) {
+  const bool upper = (threadIdx.x & S) != 0;
+  if constexpr (N == 1) {
+    v[0] += dpp<CTRL>(v[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const double mine = upper ? v[i + N / 2] : v[i], other = upper ? v[i] : v[i + N / 2];
+      v[i] = mine + dpp<CTRL>(other);
+    }
+  }
+}
+
+constexpr int pages_at_once(int heads) { return heads == 1 ? 8 : 4; }  // of a group of 16 lanes: 8 sums, or 16 for four heads
+
+template <int D, bool F32, int G>
+__global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs a, const int blocks, const int steps) {
+  constexpr int C = D / 16;                 // channels of a lane
+  constexpr int U = pages_at_once(G), V = U * G;
+  __shared__ double q_s[G][C][16];
+  const int heads = a.c.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & 15, lanes = lane >> 4;
+  const int block = (int)(blockIdx.x % (unsigned)blocks);
   unsigned unit = blockIdx.x / (unsigned)blocks;
   const int h = (int)(unit % (unsigned)heads);
   unit /= (unsigned)heads;
@@ -34,142 +68,253 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
   const int pos = a.b.lens[s] - whole + t;
   const int last = pos >= 0 ? pos >> a.c.log2_page : -1;
-  const bool open = place <= last && place < a.b.width;
-  const int p = open ? a.b.table[(int64_t)s * a.b.table_stride + place] : -1;
-  const bool there = open && p >= 0 && p < a.c.n_pages;
-  const uint16_t* const lo = a.c.bounds + ((int64_t)(there ? p : 0) * heads + h) * (2 * D);
-  float best = -INFINITY;
-  bool nan = false;
-  for (int g0 = 0; g0 < a.group; g0 += HEADS_AT_ONCE) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < HEADS_AT_ONCE * D; i += 256) {
-      const int g = g0 + i / D < a.group ? g0 + i / D : a.group - 1;
-      q_s[i / D][i % D] = (double)load_value(a.q.p, row * a.q.ld_row + (h * a.group + g) * a.q.ld_head + i % D, F32);
+  const int n = min(last + 1, a.b.width);
+  // a wavefront: `steps` times 4 U pages
+  const int first = (block * 4 + wave) * steps * (4 * U);
+  if (block * 4 * steps * (4 * U) >= n) return;  // (the whole workgroup)
+  const int32_t* const table = a.b.table + (int64_t)s * a.b.table_stride;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(a.scores) + (row * heads + h) * a.b.width;
+
+  const auto stage = [&](int g0) {
+    for (int i = threadIdx.x; i < G * D; i += 256) {
+      const int g = g0 + i / D < a.group ? g0 + i / D : a.group - 1, c = i % D;
+      q_s[i / D][c % C][c / C] = (double)load_value(a.q.p, row * a.q.ld_row + (h * a.group + g) * a.q.ld_head + c, F32);
     }
     __syncthreads();
-    double sum[HEADS_AT_ONCE] = {};
-    if (there)
-      for (int j = 0; j < D; ++j) {
-        const double x = (double)__uint_as_float((uint32_t)lo[j] << 16), y = (double)__uint_as_float((uint32_t)lo[D + j] << 16);
+  };
+  if (a.group <= G) stage(0);
+
+  for (int step = 0; step < steps; ++step) {
+    const int base = first + step * (4 * U);
+    bool there[U];
+    uint32_t lo[U][C / 2], hi[U][C / 2];
 #pragma unroll
-        for (int g = 0; g < HEADS_AT_ONCE; ++g) {
-          const double f = q_s[g][j];
-          sum[g] += f > 0. ? f * y : f * x;
+    for (int u = 0; u < U; ++u) {
+      const int place = base + 4 * u + lanes, p = place < n ? table[place] : -1;
+      there[u] = p >= 0 && p < a.c.n_pages;
+      const uint16_t* const from = a.c.bounds + ((int64_t)(there[u] ? p : 0) * heads + h) * (2 * D) + j * C;
+#pragma unroll
+      for (int c = 0; c < C / 2; c += 4 < C / 2 ? 4 : C / 2) {
+        if constexpr (C == 4) {
+          *reinterpret_cast<uint2_t*>(&lo[u][c]) = *reinterpret_cast<const uint2_t*>(from + 2 * c);
+          *reinterpret_cast<uint2_t*>(&hi[u][c]) = *reinterpret_cast<const uint2_t*>(from + D + 2 * c);
+        } else {
+          *reinterpret_cast<uint4_t*>(&lo[u][c]) = *reinterpret_cast<const uint4_t*>(from + 2 * c);
+          *reinterpret_cast<uint4_t*>(&hi[u][c]) = *reinterpret_cast<const uint4_t*>(from + D + 2 * c);
         }
       }
+    }
+    float best = -INFINITY;
+    bool nan = false;
+    for (int g0 = 0; g0 < a.group; g0 += G) {
+      if (a.group > G) {
+        __syncthreads();
+        stage(g0);
+      }
+      double sum[V] = {};
 #pragma unroll
-    for (int g = 0; g < HEADS_AT_ONCE; ++g) {
-      const float v = (float)sum[g];
+      for (int c = 0; c < C; ++c) {
+        float low[U], high[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          low[u] = __uint_as_float((c & 1) ? lo[u][c / 2] & 0xffff0000u : lo[u][c / 2] << 16);
+          high[u] = __uint_as_float((c & 1) ? hi[u][c / 2] & 0xffff0000u : hi[u][c / 2] << 16);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const double f = q_s[g][c][j];
+          const bool positive = f > 0.;
+#pragma unroll
+          for (int u = 0; u < U; ++u) sum[u * G + g] = fma(f, (double)(positive ? high[u] : low[u]), sum[u * G + g]);
+        }
+      }
+      add_halves<8, ROR8, V>(sum);
+      add_halves<4, HALF_MIRROR, V / 2>(sum);
+      add_halves<2, XOR2, V / 4>(sum);
+      add_halves<1, XOR1, V / 8>(sum);
+      // lane j (of eight sums: lanes 2 i and 2 i + 1) has the sum of page sum / G of the lane group and head sum % G
+      const float v = (float)sum[0];
       nan |= v != v;
       best = fmaxf(best, v);
     }
+    uint32_t rank = nan ? 1u : 0u;
+    if (rank == 0) {
+      const uint32_t bits = __float_as_uint(best + 0.f);
+      rank = bits ^ ((bits >> 31) ? 0xffffffffu : 0x80000000u);
+    }
+    // the best of the heads; a NaN of one is the page's
+    constexpr int HEAD_BITS = G == 1 ? 0 : G == 2 ? 2 : 3;  // lane bits that are the head's
+    const auto merge = [&](uint32_t x) { rank = rank == 1u || x == 1u ? 1u : max(rank, x); };
+    if constexpr ((HEAD_BITS & 1) != 0) merge((uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, XOR1, 0xf, 0xf, true));
+    if constexpr ((HEAD_BITS & 2) != 0) merge((uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, XOR2, 0xf, 0xf, true));
+    const int u = (V == 16 ? j : j >> 1) / G, place = base + 4 * u + lanes;
+    bool is = false;
+#pragma unroll
+    for (int i = 0; i < U; ++i) is = i == u ? there[i] : is;
+    if (place < a.keep_first || place > last - a.keep_last) rank = 0xffffffffu;
+    if ((j & (16 / U - 1)) == 0 && place < n) words[place] = is ? rank : 0u;
   }
-  if (place >= a.b.width) return;
-  uint32_t word = 0;
-  if (there) {
-    const uint32_t b = __float_as_uint(best + 0.f);
-    word = nan ? 1u : b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
-    if (place < a.keep_first || place > last - a.keep_last) word = 0xffffffffu;
-  }
-  reinterpret_cast<uint32_t*>(a.scores)[(row * heads + h) * a.b.width + place] = word;
 }
 
-template <int THREADS>
+template <int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectArgs a) {
   constexpr int WAVES = THREADS / 64;
-  __shared__ int count_s[256];
-  __shared__ int found_s[3];  // byte of the last wanted word, words above it, words of this byte
-  __shared__ int above_s[WAVES], equal_s[WAVES];
-  const int heads = a.c.heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int count_s[4][256];
+  static_assert(HELD * WAVES <= 64, "a lane for each");
+  __shared__ int sum_s[64];
+  __shared__ int kept_s[2][WAVES];
+  __shared__ uint32_t range_s[2][WAVES];
+  const int heads = a.c.heads, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   unsigned unit = blockIdx.x;
   const int h = (int)(unit % (unsigned)heads);
   unit /= (unsigned)heads;
   const int s = (int)(unit / (unsigned)a.b.max_new), t = (int)(unit % (unsigned)a.b.max_new);
-  const int whole = a.b.count(s);
+  const int whole = a.b.count(s), len = a.b.lens[s];
   const int64_t row = a.b.first_row(s) + t;
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
-  const int pos = a.b.lens[s] - whole + t;
+  const int pos = len - whole + t;
   const int n = pos >= 0 ? min((pos >> a.c.log2_page) + 1, a.b.width) : 0;
   const uint32_t* const words = reinterpret_cast<const uint32_t*>(a.scores) + (row * heads + h) * a.b.width;
   int32_t* const out = a.chosen + (row * heads + h) * a.n_chosen;
 
-  // the n_chosen-th largest word: `bar`; `room` of its equals are taken
-  uint32_t bar = 0, known = 0;
-  int room = a.n_chosen;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += THREADS) count_s[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += THREADS) {
-      const uint32_t w = words[i];
-      if (w != 0 && (w & known) == bar) atomicAdd(&count_s[(w >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      // from the highest byte down: lane holds bytes 255 - 4 lane - 0..3
+  // places tid, tid + THREADS, ..: the first HELD of a thread in registers
+  uint32_t held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < n ? words[i * THREADS + tid] : 0u;
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) f(held[i]);
+    for (int i = HELD * THREADS + tid; i < n; i += THREADS) f(words[i]);
+  };
+  for (int i = tid; i < 4 * 256; i += THREADS) count_s[i >> 8][i & 255] = 0;
+
+  // pages that are kept, others, and the others' range
+  int kept = 0, others = 0;
+  uint32_t least = 0xffffffffu, most = 0;
+  each([&](uint32_t w) {
+    const bool other = w != 0 && w != 0xffffffffu;
+    kept += w == 0xffffffffu ? 1 : 0;
+    others += other ? 1 : 0;
+    least = min(least, other ? w : 0xffffffffu), most = max(most, other ? w : 0u);
+  });
+  const auto add = [](int x, int y) { return x + y; };
+  kept = over_wavefront(kept, add), others = over_wavefront(others, add);
+  least = over_wavefront(least, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+  most = over_wavefront(most, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+  if (lane == 0) kept_s[0][wave] = kept, kept_s[1][wave] = others, range_s[0][wave] = least, range_s[1][wave] = most;
+  __syncthreads();
+  kept = others = 0;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) kept += kept_s[0][v], others += kept_s[1][v], least = min(least, range_s[0][v]), most = max(most, range_s[1][v]);
+
+  // what is taken: kept pages, words whose bits from `shift` on are above `bar`, and the first `room` places of those that equal it
+  uint32_t bar = 0;
+  int shift = 0, room = a.n_chosen - kept;
+  if (room == 0) {
+    bar = 0xffffffffu;
+  } else if (others > room) {
+    shift = least == most ? 0 : 32 - __builtin_clz(least ^ most);
+    bar = shift < 32 ? most >> shift : 0u;
+    for (int pass = 0; shift > 0; ++pass) {
+      const int bits = shift < 8 ? shift : 8, next = shift - bits;
+      each([&](uint32_t w) {
+        if (w != 0 && w != 0xffffffffu && (shift == 32 || (w >> shift) == bar)) atomicAdd(&count_s[pass][(w >> next) & ((1u << bits) - 1)], 1);
+      });
+      __syncthreads();
+      // every wavefront for itself, from the highest value down: lane holds 255 - 4 lane - 0..3
       int c[4], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = count_s[255 - 4 * lane - i], sum += c[i];
+      for (int i = 0; i < 4; ++i) c[i] = count_s[pass][255 - 4 * lane - i], sum += c[i];
       int upto = sum;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int v = __shfl_up(upto, o);
         if (lane >= o) upto += v;
       }
-      const int total = __shfl(upto, 63);
-      if (lane == 0 && total < room) found_s[0] = -1;  // fewer pages than places: all of them
-      int over = upto - sum;
+      int over = upto - sum, value = 0, here = 0, many = 0;
+      bool mine = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (over < room && over + c[i] >= room) found_s[0] = 255 - 4 * lane - i, found_s[1] = over;
+        if (over < room && over + c[i] >= room) mine = true, value = 255 - 4 * lane - i, here = over, many = c[i];
         over += c[i];
       }
+      const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine));  // one lane has it: there are at least `room` of these words
+      value = __builtin_amdgcn_readlane(value, from), here = __builtin_amdgcn_readlane(here, from), many = __builtin_amdgcn_readlane(many, from);
+      bar = (shift == 32 ? 0u : bar << bits) | (uint32_t)value;
+      room -= here;
+      shift = next;
+      if (many == room) break;  // all of them
     }
-    __syncthreads();
-    if (found_s[0] < 0) {  // (only before the first byte is known)
-      bar = 0;
-      room = 0;
-      break;
-    }
-    bar |= (uint32_t)found_s[0] << shift;
-    known |= 0xffu << shift;
-    room -= found_s[1];
-    __syncthreads();
   }
 
-  int above = 0, equal = 0;  // of the places before this block of THREADS
-  for (int i0 = 0; i0 < n; i0 += THREADS) {
-    const uint32_t w = i0 + tid < n ? words[i0 + tid] : 0;
-    const uint64_t more = __builtin_amdgcn_ballot_w64(w > bar), same = __builtin_amdgcn_ballot_w64(w == bar && w != 0);
-    __syncthreads();
-    if (lane == 0) above_s[wave] = __popcll(more), equal_s[wave] = __popcll(same);
-    __syncthreads();
-    const uint64_t before = (1ull << lane) - 1;
-    int more_before = above + __popcll(more & before), same_before = equal + __popcll(same & before);
+  const auto over = [&](uint32_t w) { return w == 0xffffffffu || (w != 0 && (w >> shift) > bar); };
+  const auto level = [&](uint32_t w) { return w != 0 && w != 0xffffffffu && (w >> shift) == bar; };
+  const uint64_t before = (1ull << lane) - 1;
+  int above = 0, equal = 0;  // of the places so far
+  for (int i0 = 0; i0 < n; i0 += HELD * THREADS) {
+    if (i0 > 0) {
 #pragma unroll
-    for (int v = 0; v < WAVES; ++v) {
-      if (v < wave) more_before += above_s[v], same_before += equal_s[v];
-      above += above_s[v];
-      equal += equal_s[v];
+      for (int i = 0; i < HELD; ++i) held[i] = i0 + i * THREADS + tid < n ? words[i0 + i * THREADS + tid] : 0u;
     }
-    const bool take = w > bar || (w == bar && w != 0 && same_before < room);
-    if (take) out[more_before + min(same_before, room)] = i0 + tid;
+    __syncthreads();
+    // 64 places each in the order of the places: those above the bar in the lower half of a word, its equals in the upper
+    uint64_t more[HELD], same[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      more[i] = __builtin_amdgcn_ballot_w64(over(held[i])), same[i] = __builtin_amdgcn_ballot_w64(level(held[i]));
+      if (lane == 0) sum_s[i * WAVES + wave] = __popcll(more[i]) | __popcll(same[i]) << 16;
+    }
+    __syncthreads();
+    const int own = lane < HELD * WAVES ? sum_s[lane] : 0;
+    int upto = own;
+#pragma unroll
+    for (int o = 1; o < HELD * WAVES; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, HELD * WAVES - 1);
+    upto -= own;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int start = __builtin_amdgcn_readlane(upto, i * WAVES + wave);
+      const int more_before = above + (start & 0xffff) + __popcll(more[i] & before), same_before = equal + (start >> 16) + __popcll(same[i] & before);
+      if (over(held[i]) || (level(held[i]) && same_before < room)) out[more_before + min(same_before, room)] = i0 + i * THREADS + tid;
+    }
+    above += all & 0xffff, equal += all >> 16;
   }
   for (int i = above + min(equal, room) + tid; i < a.n_chosen; i += THREADS) out[i] = -1;
+}
+
+template <int D, bool F32, int G>
+hipError_t launch_score(const PagesSelectArgs& a, int64_t units, hipStream_t s) {
+  // a wavefront takes a step (16 or 32 pages), up to eight where that leaves three workgroups for a compute unit.  Four rows of 8 heads and
+  // 2048 pages, both kernels: one 25.2 us, two 21.2, three and more 19.3
+  constexpr int per = 4 * 4 * pages_at_once(G);
+  const int64_t all = (a.b.width + per - 1) / per;
+  int64_t steps = units * all / (3 * device_cu_count());
+  steps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
+  const int64_t blocks = (all + steps - 1) / steps;
+  hipLaunchKernelGGL((pages_score_kernel<D, F32, G>), dim3((unsigned)(units * blocks)), dim3(256), 0, s, a, (int)blocks, (int)steps);
+  return hipGetLastError();
+}
+template <int D, bool F32>
+hipError_t launch_score_g(const PagesSelectArgs& a, int64_t units, hipStream_t s) {
+  if (a.group == 1) return launch_score<D, F32, 1>(a, units, s);
+  if (a.group == 2) return launch_score<D, F32, 2>(a, units, s);
+  return launch_score<D, F32, 4>(a, units, s);
 }
 
 template <int D>
 hipError_t launch(bool f32, const PagesSelectArgs& a, hipStream_t s) {
   const int64_t units = (int64_t)a.b.n_seqs * a.b.max_new * a.c.heads;
-  const int blocks = (a.b.width + 255) / 256;
-  const dim3 grid((unsigned)(units * blocks));
-  if (blocks > 0) {
-    if (f32) hipLaunchKernelGGL((pages_score_kernel<D, true>), grid, dim3(256), 0, s, a, blocks);
-    else hipLaunchKernelGGL((pages_score_kernel<D, false>), grid, dim3(256), 0, s, a, blocks);
-    const hipError_t e = hipGetLastError();
+  if (a.b.width > 0) {
+    const hipError_t e = f32 ? launch_score_g<D, true>(a, units, s) : launch_score_g<D, false>(a, units, s);
     if (e != hipSuccess) return e;
   }
-  if (a.b.width > 2048) hipLaunchKernelGGL((pages_pick_kernel<1024>), dim3((unsigned)units), dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((pages_pick_kernel<256>), dim3((unsigned)units), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)units);
+  if (a.b.width > 4096) hipLaunchKernelGGL((pages_pick_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
+  else if (a.b.width > 1024) hipLaunchKernelGGL((pages_pick_kernel<512, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((pages_pick_kernel<256, 4>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

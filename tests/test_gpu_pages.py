@@ -304,6 +304,9 @@ SELECT = [
     (64, 16, "f32", 1, 3, [700, 100], [4, 1], 7, 0, 0),
     (256, 32, "bf16", 3, 1, [900, 31], [2, 2], 40, 2, 3),
     (64, 16, "bf16", 1, 16, [4000], [1], 64, 1, 2),
+    (128, 16, "f32", 2, 2, [333, 20], [1, 3], 5, 2, 3),   # no room for others
+    (128, 16, "bf16", 1, 5, [3, 0], [5, 2], 2, 0, 1),     # rows before the first token
+    (256, 16, "f32", 1, 2, [20000], [1], 200, 0, 1),
 ]
 
 
@@ -314,7 +317,8 @@ def test_select(case):
     b = Batch(rng, lens, new, page)
     bounds = torch.from_numpy(np.sort(rng.standard_normal((b.n_pages, heads, 2, d)), 2)).to(DEV, torch.bfloat16)
     longest = b.table[int(np.argmax(lens))]
-    bounds[longest[0]] = bounds[longest[2]]  # equal scores
+    if max(lens) > 2 * page:
+        bounds[longest[0]] = bounds[longest[2]]  # equal scores
     zero = torch.zeros((b.n_pages, heads, page, d), dtype=torch.int8, device=DEV)
     ones = torch.ones((b.n_pages, heads), device=DEV)
     p = tq.Pages(zero, zero, ones, ones, bounds=bounds)
