@@ -496,7 +496,7 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *   Scales  tq_pages_append makes powers of two: the smallest 2^e with amax / 2^e <= 448 (127), e in [-40, 40], amax over
  *           the block's finite values; larger values (infinities among them) take the largest code, NaN takes NaN (int8: 0).
  *           A power of two lets a block whose scale grows be coded again without a second rounding of what stays
- *           representable.  tq_pages_attend takes any positive scales.
+ *           representable.  tq_pages_attend takes any positive scales (2^-126 to 2^125).
  *   Bounds  (optional) the smallest and largest value of every channel of a page's keys, rounded outward to bf16.
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
@@ -538,7 +538,7 @@ typedef struct tq_batch {
  * Store the new keys and values.  k, v: device, n_rows rows (dtype TQ_F32 or TQ_BF16) of n_heads vectors, `ld_row` elements
  * between rows and `ld_head` between heads; 16-byte aligned, strides multiples of 16 bytes, else TQ_ERR_UNSUPPORTED.
  * A page whose first token is among the new ones starts afresh; in any other the scale grows to max(old, new) and the codes
- * that were there are rounded to it.  Slots behind the last token stay as they were.  Two sequences of one call must not
+ * that were there are rounded to it (an old one that is no power of two is first taken up to one).  Slots behind the last token stay as they were.  Two sequences of one call must not
  * store into the same page.  No workspace.
  */
 tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, const void* v, int32_t dtype, int64_t ld_row,

@@ -16,6 +16,8 @@ namespace {
 constexpr int HELD = 4;
 constexpr float BF16_MAX = 3.38953139e38f;
 
+typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+
 template <bool F32>
 struct Vec8 {
   uint4_t w[F32 ? 2 : 1];
@@ -27,6 +29,20 @@ struct Vec8 {
       w[0] = *reinterpret_cast<const uint4_t*>(static_cast<const uint16_t*>(p) + at);
     }
   }
+  // the larger of `most` and the values' magnitudes: of fp32 their bits; of bf16 two at a time, to be taken apart by unpacked()
+  __device__ __forceinline__ uint32_t top(uint32_t most) const {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, w[i >> 2][i & 3] & 0x7fffffffu);
+      return most;
+    } else {
+      ushort2_t m = __builtin_bit_cast(ushort2_t, most);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2_t, w[0][i] & 0x7fff7fffu));
+      return __builtin_bit_cast(uint32_t, m);
+    }
+  }
+  static __device__ __forceinline__ uint32_t unpacked(uint32_t most) { return F32 ? most : max(most & 0xffff0000u, most << 16); }
   __device__ __forceinline__ float operator[](int i) const {
     if constexpr (F32) return __uint_as_float(w[i >> 2][i & 3]);
     else return __uint_as_float((i & 1) ? w[0][i >> 1] & 0xffff0000u : w[0][i >> 1] << 16);
@@ -57,7 +73,7 @@ template <int D, int CT, bool F32, int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_append_kernel(const PagesView c, const BatchView b, const PagesRows kr, const PagesRows vr,
                                                               const int pages_each) {
   constexpr int COLS = D / 8, LINES = THREADS / COLS;  // threads of a row, rows at a time
-  __shared__ float red_s[THREADS / 64];
+  __shared__ uint32_t red_s[THREADS / 64];
   __shared__ float edge_s[2][LINES][D];
   const int tid = threadIdx.x, col = tid % COLS, line = tid / COLS;
   const int s = (int)(blockIdx.x / (unsigned)pages_each), h = blockIdx.y;
@@ -84,12 +100,14 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const PagesView c
   const PagesRows& x = values ? vr : kr;
   const int64_t from = (row0 + (lo - begin)) * x.ld_row + h * x.ld_head + 8 * col;
   const int mine = rows > line ? (rows - line + LINES - 1) / LINES : 0;  // vectors of this thread: rows line, line + LINES, ...
+  const bool bounds = !values && c.bounds != nullptr;
 
+  // the largest magnitude, as bits (those of what is not finite above all others), and of keys the channels' ends
   Vec8<F32> held[HELD];
-  float amax = 0.f, low[8], high[8];
+  uint32_t top = 0;
+  float low[8], high[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) low[i] = INFINITY, high[i] = -INFINITY;
-  const bool bounds = !values && c.bounds != nullptr;
   for (int j0 = 0; j0 < mine; j0 += HELD) {
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
@@ -97,30 +115,49 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const PagesView c
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
       if (j0 + u < mine) {
+        top = held[u].top(top);
+        if (bounds)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = held[u][i], m = fabsf(y);
-          amax = fmaxf(amax, m <= FLT_MAX ? m : 0.f);
-          low[i] = fminf(low[i], y);  // (a NaN is passed over)
-          high[i] = fmaxf(high[i], y);
-        }
+          for (int i = 0; i < 8; ++i) low[i] = fminf(low[i], held[u][i]), high[i] = fmaxf(high[i], held[u][i]);  // (a NaN is passed over)
       }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-  if ((tid & 63) == 0) red_s[tid >> 6] = amax;
+  top = Vec8<F32>::unpacked(top);
+  const auto larger = [](uint32_t p, uint32_t q) { return p > q ? p : q; };
+  top = over_wavefront(top, larger);
+  if ((tid & 63) == 0) red_s[tid >> 6] = top;
   if (bounds)
 #pragma unroll
     for (int i = 0; i < 8; ++i) edge_s[0][line][8 * col + i] = low[i], edge_s[1][line][8 * col + i] = high[i];
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) amax = fmaxf(amax, red_s[w]);
-  const float fresh = pow2(scale_exponent<CT>(amax));
-  const float after = fmaxf(fresh, before);
+  for (int w = 0; w < THREADS / 64; ++w) top = larger(top, red_s[w]);
+  const bool clean = top < 0x7f800000u;  // every value is finite
+  float amax = __uint_as_float(top);
+  if (!clean) {
+    amax = 0.f;
+    for (int j = 0; j < mine; ++j) {
+      held[0].load(x.p, from + (int64_t)(line + j * LINES) * x.ld_row);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(held[0][i]) <= FLT_MAX ? fabsf(held[0][i]) : 0.f);
+    }
+    amax = over_wavefront(amax, [](float p, float q) { return fmaxf(p, q); });
+    __syncthreads();
+    if ((tid & 63) == 0) red_s[tid >> 6] = __float_as_uint(amax);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) amax = fmaxf(amax, __uint_as_float(red_s[w]));
+  }
+  // a power of two: what was there (of any kind, if append has not made it) is taken up to one
+  const uint32_t was = __float_as_uint(before);
+  const bool old = had > 0 && was >= 0x00800000u && was < 0x7e800000u;
+  int e = scale_exponent<CT>(amax);
+  const bool beyond = e == kPageScaleHigh;  // (values may be larger than the largest code)
+  if (old) e = max(e, (int)(was >> 23) - 127 + ((was & 0x7fffffu) != 0 ? 1 : 0));
+  const float after = pow2(e), inv = pow2(-e);
   if (tid == 0) *scale = after;
 
-  if (had > 0 && after > before) {
-    const float factor = before / after;
+  if (old && after != before) {
+    const float factor = before * inv;
     for (int i = tid * 16; i < had * D; i += THREADS * 16) {
       uint4_t w = *reinterpret_cast<const uint4_t*>(codes + i);
 #pragma unroll
@@ -128,29 +165,45 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const PagesView c
         float y[4];
         page_decode<CT>(w[j], y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] *= factor;
+        for (int k = 0; k < 4; ++k) y[k] *= factor;
         w[j] = page_encode<CT>(y);
       }
       *reinterpret_cast<uint4_t*>(codes + i) = w;
     }
   }
 
-  const float inv = 1.f / after;  // (before may be any positive scale)
-  const bool power = (__float_as_uint(after) & 0x7fffffu) == 0;
-  for (int j0 = 0; j0 < mine; j0 += HELD) {
+  const auto store = [&](auto encode) {
+    for (int j0 = 0; j0 < mine; j0 += HELD) {
+      if (mine > HELD || !clean) {
 #pragma unroll
-    for (int u = 0; u < HELD; ++u)
-      if (j0 + u < mine) {
-        const int row = line + (j0 + u) * LINES;
-        if (mine > HELD) held[u].load(x.p, from + (int64_t)row * x.ld_row);
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = power ? held[u][i] * inv : held[u][i] / after;
-        uint2_t w;
-        w[0] = page_encode<CT>({y[0], y[1], y[2], y[3]});
-        w[1] = page_encode<CT>({y[4], y[5], y[6], y[7]});
-        *reinterpret_cast<uint2_t*>(codes + (int64_t)(had + row) * D + 8 * col) = w;
+        for (int u = 0; u < HELD; ++u)
+          if (j0 + u < mine) held[u].load(x.p, from + (int64_t)(line + (j0 + u) * LINES) * x.ld_row);
       }
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+        if (j0 + u < mine) {
+          uint2_t w;
+          w[0] = encode(held[u][0], held[u][1], held[u][2], held[u][3]);
+          w[1] = encode(held[u][4], held[u][5], held[u][6], held[u][7]);
+          *reinterpret_cast<uint2_t*>(codes + (int64_t)(had + line + (j0 + u) * LINES) * D + 8 * col) = w;
+        }
+    }
+  };
+  if (clean && !beyond) {
+    store([&](float p, float q, float r, float t) {
+      if constexpr (CT == kPageE4m3) {
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(p * inv, q * inv, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(r * inv, t * inv, w, true);
+      } else {
+        // 1.5 * 2^23 above: the sum is rounded to a whole number, ties to even, whose two's complement ends its bits
+        constexpr float up = 12582912.f;
+        const uint32_t a0 = __float_as_uint(fmaf(p, inv, up)), a1 = __float_as_uint(fmaf(q, inv, up));
+        const uint32_t a2 = __float_as_uint(fmaf(r, inv, up)), a3 = __float_as_uint(fmaf(t, inv, up));
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(a3, a2, 0x0c0c0400u), __builtin_amdgcn_perm(a1, a0, 0x0c0c0400u), 0x05040100u);
+      }
+    });
+  } else {
+    store([&](float p, float q, float r, float t) { return page_encode<CT>({p * inv, q * inv, r * inv, t * inv}); });
   }
 
   if (bounds)

@@ -299,6 +299,25 @@ def test_scales_and_codes_on_either_side_of_a_step(kind):
         assert np.array_equal(got[name], want[name], equal_nan=True), (name, np.argwhere(~((got[name] == want[name]) | np.isnan(want[name])))[:5])
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_a_scale_that_append_has_not_made(kind):
+    """It is taken up to a power of two; what was there moves by half a step of its code at most (and u of the product before)."""
+    rng = np.random.default_rng(51)
+    p = tq.make_pages(2, 1, 64, 16, dtype=KINDS[kind], device=DEV)
+    p.k.copy_(random_codes(rng, p.k.shape, kind, False)), p.v.copy_(p.k)
+    p.k_scale.fill_(0.3), p.v_scale.fill_(3.0)
+    before = cache64(p)
+    x = torch.from_numpy(rng.standard_normal((1, 1, 64)).astype(np.float32)).to(DEV)
+    tq.tq_pages_append(p, x, x, ints([[1]]), ints([11]), None, 1)
+    got = cache64(p)
+    assert got["k_scale"][1, 0] == 0.5 and got["v_scale"][1, 0] == 4.0
+    for name, to in (("k", 0.5), ("v", 4.0)):
+        was = before[name][1, 0, :10] * before[name + "_scale"][1, 0]
+        step = to * (1.0 if kind == "int8" else np.maximum(2.0**-9, 2.0**-3 * np.abs(was / to)))
+        assert (np.abs(got[name][1, 0, :10] * to - was) <= step / 2 * (1 + 2.0**-20) + 2.0**-23 * np.abs(was)).all()
+        assert np.array_equal(got[name][1, 0, 11:], before[name][1, 0, 11:]) and np.array_equal(got[name][0], before[name][0])
+
+
 SELECT = [
     (128, 64, "bf16", 2, 4, [1, 64, 65, 2000], [1, 1, 1, 1], 5, 1, 1),
     (64, 16, "f32", 1, 3, [700, 100], [4, 1], 7, 0, 0),
