@@ -80,7 +80,7 @@ struct PagesAttendArgs {
   const int32_t* chosen;
   int n_chosen;
   int group;  // query heads that read a head of the cache
-  float scale;
+  float scale2, scale2_rest;  // log2(e) scale as a sum of two
   int window;  // of tokens that a row sees; INT_MAX: all
   int splits;   // ranges that the keys of a unit are cut into
   bool prompt;  // the kernel for prompts

@@ -158,7 +158,9 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
   a.c = view(c), a.b = view(b);
   a.q = PagesRows{q, ldq_row, ldq_head}, a.out = PagesRows{out, ldo_row, ldo_head};
   a.lse = lse, a.chosen = chosen, a.n_chosen = n_chosen, a.group = n_heads_q / c->n_heads;
-  a.scale = scale, a.window = window > 0 ? window : INT_MAX;
+  const double scale2 = (double)scale * 1.4426950408889634074;
+  a.scale2 = (float)scale2, a.scale2_rest = (float)(scale2 - (double)a.scale2);
+  a.window = window > 0 ? window : INT_MAX;
   if (!attend_fits(b, c->n_heads, a.group, chosen != nullptr)) return TQ_ERR_UNSUPPORTED;
   PagesAttendPlan plan;
   const size_t need = attend_part_bytes(c, b, dtype == TQ_F32, a.group, chosen != nullptr, n_chosen, window, &plan);

@@ -61,7 +61,6 @@ struct Walk {
   bf16x8_t q[R][QP][KS];
   float4_t o[R][VE];
   float l[R], M[R], shift[R], limit[R];  // shift = BASE - M, limit: of x before a new M is taken
-  float c_hi, c_lo;
 
   __device__ __forceinline__ explicit Walk(const PagesAttendArgs& args) : a(args) {}
 
@@ -105,8 +104,6 @@ struct Walk {
     table = a.b.table + (int64_t)s * a.b.table_stride;
     list = a.chosen != nullptr ? a.chosen + ((row0 + t0) * heads + h) * a.n_chosen : nullptr;
     listed = a.chosen == nullptr || (row0 + t0 >= 0 && row0 + t0 < a.b.n_rows);
-    const double c64 = (double)a.scale * 1.4426950408889634074;
-    c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
     return true;
   }
   __device__ __forceinline__ int tiles() const { return hi > lo ? (hi - lo + 31) >> 5 : 0; }
@@ -154,12 +151,10 @@ struct Walk {
 
   __device__ __forceinline__ void load(Tile<D>& b, int i) {
     if (((i - begin) & 31) == 0) look_up(i);
+    const int from = ((i - begin) & 31) << 1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int from = (((i - begin) & 31) << 1) + u;
-      const int at = __builtin_amdgcn_readlane(sub.at, from);
-      b.pos[u] = __builtin_amdgcn_readlane(sub.pos, from);
-      b.ks[u] = lane_value(sub.ks, from), b.lv[u] = lane_value(sub.lv, from), b.iv[u] = lane_value(sub.iv, from);
+      const int at = __builtin_amdgcn_readlane(sub.at, from + u);
       const int64_t off = (int64_t)(at < 0 ? 0 : at) * (16 * D);  // where there is no page, the pool's first bytes, unused
       const uint8_t* const kp = a.c.k + off + r * D + g * (D / 4);
 #pragma unroll
@@ -173,13 +168,20 @@ struct Walk {
         if constexpr (D == 256) *reinterpret_cast<uint4_t*>(to) = *reinterpret_cast<const uint4_t*>(vp + j * D);
       }
     }
+    // (behind the loads: these wait for the scales)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      b.pos[u] = __builtin_amdgcn_readlane(sub.pos, from + u);
+      b.ks[u] = lane_value(sub.ks, from + u), b.lv[u] = lane_value(sub.lv, from + u), b.iv[u] = lane_value(sub.iv, from + u);
+    }
   }
 
   // x of row tile i: base-2 logarithms of its weights in the frame
   __device__ __forceinline__ void exponents(float (&x)[8], const float4_t (&acc)[2], const Tile<D>& b, int i, uint32_t hidden) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const float ch = b.ks[u] * c_hi, cl = b.ks[u] * c_lo, add = b.lv[u] + shift[i];
+      const float ch = b.ks[u] * a.scale2, cl = b.ks[u] * a.scale2_rest, add = b.lv[u] + shift[i];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         x[4 * u + e] = fmaf(acc[u][e], ch, add);

@@ -163,7 +163,6 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   float l = 0.f, M = -INFINITY, shift = 0.f, limit = -3e38f;
-  const float c2 = (float)((double)a.scale * 1.4426950408889634074);
 
   // where not all of the workgroup's rows see all of a tile: its subtiles' positions from the lanes that know them
   const auto tile_pos = [&](int tile, int u) { return __builtin_amdgcn_readlane(sub.pos, ((tile & 15) << 2) + u); };
@@ -208,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
       const auto exponents = [&] {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float ch = ks[2 * kt + u] * c2, add = lv[2 * kt + u] + shift;
+          const float ch = ks[2 * kt + u] * a.scale2, add = lv[2 * kt + u] + shift;
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[8 * u + i] = fmaf(acc[8 * u + i], ch, add);
         }
