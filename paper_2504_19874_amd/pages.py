@@ -98,7 +98,7 @@ def _ints(t, what, shape, device):
 
 def _batch(p: Pages, n_rows: int, table, lens, starts, max_new: int):
     _where(table, "table")
-    if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.device != p.device:
+    if table.dtype != torch.int32 or table.dim() != 2 or (table.numel() and table.shape[1] > 1 and table.stride(1) != 1) or table.device != p.device:
         raise TurboQuantError(f"table: expected int32 [n_seqs][width] with contiguous rows on {p.device}, got {table.dtype} {tuple(table.shape)}")
     n, width = table.shape
     if n > 1 and table.stride(0) < width:

@@ -1,0 +1,306 @@
+"""The paged 8-bit cache as a serving program uses it: its operators one after another, captured and replayed, on views of wider
+arrays, on another stream, at addresses beyond 32 bits, and through the binding without its compiled half."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages_oracle as po
+from tests import test_gpu_pages as T
+
+pytestmark = pytest.mark.gpu
+
+tq = pytest.importorskip("paper_2504_19874_amd")
+
+DEV, ints = T.DEV, T.ints
+
+
+class Server:
+    """Four sequences, 2 heads of the cache and 6 of the queries, d = 64, pages of 16; what the oracle thinks beside it."""
+
+    heads, group, d, page, rows, width = 2, 3, 64, 16, 4, 12
+
+    def __init__(self, kind, n_pages=30, seed=0):
+        self.kind, self.rng = kind, np.random.default_rng([61, seed])
+        self.p = tq.make_pages(n_pages, self.heads, self.d, self.page, dtype=T.KINDS[kind], bounds=True, device=DEV)
+        self.table, self.lens = ints(np.full((self.rows, self.width), -1)), ints(np.zeros(self.rows))
+        self.pool = po.Pool(np.full((self.rows, self.width), -1), np.zeros(self.rows, int), np.zeros(n_pages, int), self.page)
+        self.cache = T.cache64(self.p)
+
+    def vectors(self, n, heads):
+        return torch.from_numpy(self.rng.standard_normal((n, heads, self.d)).astype(np.float32)).to(DEV, torch.bfloat16)
+
+    def starts(self, new):
+        return [0] + np.cumsum(new).tolist()
+
+    def step(self, new, chosen=0):
+        """new[s] tokens of every sequence: their pages, their keys and values, and what they attend to."""
+        starts = self.starts(new)
+        n, most = starts[-1], max(new)
+        self.lens += ints(new)
+        k, v, q = self.vectors(n, self.heads), self.vectors(n, self.heads), self.vectors(n, self.heads * self.group)
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+        missing = ints([-1])
+        tq.tq_pages_reserve(self.p, self.table, self.lens, most, missing=missing)
+        tq.tq_pages_append(self.p, k, v, self.table, self.lens, ints(starts), most)
+        pick = None
+        if chosen:
+            pick = torch.empty((n, self.heads, chosen), dtype=torch.int32, device=DEV)
+            tq.tq_pages_select(self.p, q, self.table, self.lens, ints(starts), most, pick)
+        tq.tq_pages_attend(self.p, q, self.table, self.lens, ints(starts), most, 0.125, out, lse=lse, chosen=pick)
+        # the oracle
+        self.pool.lens += np.array(new)
+        assert self.pool.reserve(most) == int(missing)
+        table, lens = self.pool.table.tolist(), self.pool.lens.tolist()
+        po.append(self.cache, self.kind, self.page, *[t.double().cpu().numpy() for t in (k, v)], table, lens, starts)
+        if chosen:
+            q64 = q.double().cpu().numpy()
+            want = po.select(self.cache["lower"], self.cache["upper"], self.page, q64, table, lens, starts, chosen, 1, 1)
+            assert np.array_equal(pick.cpu().numpy(), want)
+        want = po.attend(self.cache, self.page, q.double().cpu().numpy(), table, lens, starts, 0.125, chosen=pick.cpu().numpy() if chosen else None)
+        T.check_attend(out, lse, want, max(lens), torch.bfloat16)
+        self.check()
+
+    def move(self, pairs):
+        for name in self.cache:
+            self.cache[name][[d for _, d in pairs]] = self.cache[name][[s for s, _ in pairs]]
+
+    def check(self):
+        assert T.same_pool(self.p, self.pool, self.table, self.lens)
+        got = T.cache64(self.p)
+        live = self.pool.refs > 0
+        for name in got:
+            assert np.array_equal(got[name][live], self.cache[name][live]), name
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_a_serving_run(kind):
+    s = Server(kind)
+    s.step([40, 3, 0, 0])                     # two prompts
+    for _ in range(3):
+        s.step([1, 1, 0, 0])
+    pairs, _ = s.pool.fork([0, 1], [2, 3])    # another answer to each
+    tq.tq_pages_fork(s.p, s.table, s.lens, ints([0, 1]), ints([2, 3]))
+    s.move(pairs)
+    s.check()
+    for i in range(14):                       # past the ends of pages; the shared ones stay as they are
+        s.step([1, 1, 1, 1], chosen=3 if i % 2 else 0)
+    s.pool.free([0])
+    tq.tq_pages_free(s.p, s.table, s.lens, ints([0]))
+    pairs, _ = s.pool.compact()
+    tq.tq_pages_compact(s.p, s.table)
+    s.move(pairs)
+    s.check()
+    s.step([30, 2, 1, 5], chosen=2)           # the row begins again, in pages that others have used
+    s.step([1, 1, 1, 1])
+
+
+def test_a_pool_that_runs_out():
+    """Tokens without a page are not stored and not there; what has one is as ever."""
+    s = Server("e4m3", n_pages=4, seed=1)
+    s.step([40, 30, 0, 0])
+    s.step([1, 1, 0, 0])
+
+
+@pytest.mark.parametrize("new", [1, 5])
+def test_captured_and_replayed(new):
+    """A decoding step in a graph: lengths advance on the GPU, and every replay is compared with the same calls made eagerly."""
+    rng = np.random.default_rng([62, new])
+    heads, group, d, page, seqs, width = 4, 2, 128, 16, 3, 300
+
+    def state():
+        p = tq.make_pages(2 * seqs * width, heads, d, page, bounds=True, device=DEV)
+        return p, ints(np.full((seqs, width), -1)), ints([0] * seqs)
+
+    x = [torch.zeros((seqs * new, n, d), dtype=torch.bfloat16, device=DEV) for n in (heads, heads, heads * group)]
+
+    def call(p, table, lens, out, lse, pick):
+        lens.add_(new)
+        tq.tq_pages_reserve(p, table, lens, new)
+        tq.tq_pages_append(p, x[0], x[1], table, lens, None, new)
+        tq.tq_pages_select(p, x[2], table, lens, None, new, pick)
+        tq.tq_pages_attend(p, x[2], table, lens, None, new, 0.1, out[0], lse=lse[0])
+        tq.tq_pages_attend(p, x[2], table, lens, None, new, 0.1, out[1], lse=lse[1], chosen=pick)
+
+    results = []
+    for _ in range(2):
+        results.append(([torch.zeros_like(x[2]) for _ in range(2)], [torch.zeros((seqs * new, heads * group), device=DEV) for _ in range(2)],
+                        torch.zeros((seqs * new, heads, 4), dtype=torch.int32, device=DEV)))
+    a, b = state(), state()
+    for p, table, _ in (a, b):
+        p.reserve_pool(), p.reserve_select(seqs * new, seqs, width, new)
+        p.reserve_attend(seqs * new, seqs, width, heads * group, new), p.reserve_attend(seqs * new, seqs, width, heads * group, new, n_chosen=4)
+    call(*b, *results[1])  # (modules are loaded before the capture)
+    for t in (*b[1:], b[0].refs):
+        t.zero_() if t is not b[1] else t.fill_(-1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*a, *results[0])
+    for i in range(40):
+        for t in x:
+            t.copy_(torch.from_numpy(rng.standard_normal(t.shape).astype(np.float32)))
+        graph.replay()
+        call(*b, *results[1])
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+        for r in range(2):
+            assert torch.equal(results[0][0][r], results[1][0][r]) and torch.equal(results[0][1][r], results[1][1][r]), i
+        assert torch.equal(results[0][2], results[1][2]) and torch.equal(a[1], b[1]) and torch.equal(a[2], b[2]) and torch.equal(a[0].refs, b[0].refs)
+    assert torch.equal(a[0].k.view(torch.uint8), b[0].k.view(torch.uint8)) and torch.equal(a[0].bounds, b[0].bounds)
+
+
+def test_views_of_wider_arrays():
+    """Queries, keys and values inside one array of a projection, outputs with gaps, table rows of a wider table, heads first."""
+    rng = np.random.default_rng(63)
+    heads, group, d, page = 2, 4, 128, 32
+    b = T.Batch(rng, [70, 33, 5], [6, 33, 1], page)
+    p = T.filled(rng, b, heads, d, "e4m3")
+    bounds = torch.zeros((b.n_pages, heads, 2, d), dtype=torch.bfloat16, device=DEV)
+    p = tq.Pages(p.k, p.v, p.k_scale, p.v_scale, bounds=bounds)
+    qkv = torch.from_numpy(rng.standard_normal((b.rows, heads * (group + 2), d + 8)).astype(np.float32)).to(DEV, torch.bfloat16)[:, :, :d]
+    q, k, v = qkv[:, :heads * group], qkv[:, heads * group:heads * (group + 1)], qkv[:, heads * (group + 1):]
+    table, lens, starts, most = b.args()
+    wide = torch.full((len(b.lens), table.shape[1] + 9), -1, dtype=torch.int32, device=DEV)
+    wide[:, 2:2 + table.shape[1]] = table
+    view = wide[:, 2:2 + table.shape[1]]
+    plain = tq.Pages(*[t.clone() for t in (p.k, p.v, p.k_scale, p.v_scale)], bounds=bounds.clone())
+    tq.tq_pages_append(p, k, v, view, lens, starts, most)
+    tq.tq_pages_append(plain, k.contiguous(), v.contiguous(), table, lens, starts, most)
+    assert torch.equal(p.k.view(torch.uint8), plain.k.view(torch.uint8)) and torch.equal(p.v.view(torch.uint8), plain.v.view(torch.uint8))
+    assert torch.equal(p.bounds, plain.bounds) and torch.equal(p.k_scale.nan_to_num(), plain.k_scale.nan_to_num())
+    want = torch.empty((b.rows, heads * group, d), dtype=torch.bfloat16, device=DEV)
+    tq.tq_pages_attend(plain, q.contiguous(), table, lens, starts, most, 0.1, want)
+    outs = [torch.full((b.rows + 1, heads * group + 1, d + 8), 7.0, dtype=torch.bfloat16, device=DEV),
+            torch.full((heads * group, b.rows, d), 7.0, dtype=torch.bfloat16, device=DEV)]
+    got = [outs[0][:b.rows, :heads * group, :d], outs[1].transpose(0, 1)]
+    for o in got:
+        tq.tq_pages_attend(p, q, view, lens, starts, most, 0.1, o)
+        assert torch.equal(o, want)
+    assert (outs[0][b.rows] == 7).all() and (outs[0][:, -1] == 7).all() and (outs[0][:, :, d:] == 7).all()
+    chosen = [torch.empty((b.rows, heads, 2), dtype=torch.int32, device=DEV) for _ in range(2)]
+    tq.tq_pages_select(p, q, view, lens, starts, most, chosen[0])
+    tq.tq_pages_select(plain, q.contiguous(), table, lens, starts, most, chosen[1])
+    assert torch.equal(*chosen)
+
+
+def test_rows_of_no_sequence_are_left_alone():
+    rng = np.random.default_rng(64)
+    for new in ([1, 1], [70, 66]):
+        b = T.Batch(rng, [90, 80], new, 16)
+        p = T.filled(rng, b, 8, 128, "int8")
+        table, lens, starts, most = b.args()
+        q = torch.from_numpy(rng.standard_normal((b.rows + 3, 8, 128)).astype(np.float32)).to(DEV, torch.bfloat16)
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV)
+        tq.tq_pages_attend(p, q, table, lens, starts + 2, most, 0.1, out, lse=lse)
+        assert (out[:2] == 7).all() and (out[-1] == 7).all() and (lse[:2] == 7).all() and (lse[-1] == 7).all() and not (out[2:-1] == 7).all()
+        # starts beyond the arrays: those rows are skipped
+        tq.tq_pages_attend(p, q, table, lens, starts + b.rows, most, 0.1, torch.empty_like(q))
+        tq.tq_pages_attend(p, q, table, lens, starts - b.rows - 5, most, 0.1, torch.empty_like(q))
+        k = torch.zeros((b.rows + 3, 8, 128), dtype=torch.bfloat16, device=DEV)
+        before = p.k.clone()
+        tq.tq_pages_append(p, k, k, table, lens, starts + b.rows + 3, most)
+        assert torch.equal(p.k, before)
+
+
+def test_another_stream():
+    rng = np.random.default_rng(65)
+    b = T.Batch(rng, [3000, 1], [1, 1], 64)
+    p = T.filled(rng, b, 4, 128, "e4m3")
+    args = b.args()
+    q = torch.from_numpy(rng.standard_normal((b.rows, 16, 128)).astype(np.float32)).to(DEV, torch.bfloat16)
+    out, other = torch.empty_like(q), torch.zeros_like(q)
+    tq.tq_pages_attend(p, q, *args, 0.1, out)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(2000000)
+        late = q.clone()
+        tq.tq_pages_attend(p, late, *args, 0.1, other)
+    s.synchronize()
+    assert torch.equal(out, other)
+
+
+@pytest.mark.parametrize("new,group", [(1, 2), (80, 1)])
+def test_addresses_beyond_32_bits(new, group):
+    """A pool of 5 GB of keys and as many values, its last pages in use."""
+    heads, d, page, n = 8, 128, 64, 80000
+    k = torch.zeros((n, heads, page, d), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    v = torch.zeros((n, heads, page, d), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    assert k.numel() > 2**32
+    rng = np.random.default_rng([66, new])
+    p = tq.Pages(k, v, torch.ones((n, heads), device=DEV), torch.ones((n, heads), device=DEV),
+                 bounds=torch.zeros((n, heads, 2, d), dtype=torch.bfloat16, device=DEV), refs=torch.zeros(n, dtype=torch.int32, device=DEV))
+    seqs = 16
+    tables = [rng.permutation(np.arange(n - 60, n))[:3 * seqs].reshape(seqs, 3), np.arange(3 * seqs).reshape(seqs, 3)]
+    lens, rows = ints([150] * seqs), seqs * 150
+    x = [torch.from_numpy(rng.standard_normal((rows, heads, d)).astype(np.float32)).to(DEV, torch.bfloat16) for _ in range(2)]
+    q = torch.from_numpy(rng.standard_normal((seqs * new, heads * group, d)).astype(np.float32)).to(DEV, torch.bfloat16)
+    out = []
+    for t in tables:
+        tq.tq_pages_append(p, *x, ints(t), lens, None, 150)
+        out.append([torch.empty_like(q), torch.empty((seqs * new, heads, 2), dtype=torch.int32, device=DEV)])
+        tq.tq_pages_attend(p, q, ints(t), lens, None, new, 0.1, out[-1][0])
+        tq.tq_pages_select(p, q, ints(t), lens, None, new, out[-1][1])
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    tq.tq_pages_copy(p, ints([n - 1, tables[0][0][0]]), ints([60, 61]))
+    assert torch.equal(p.k[60].view(torch.uint8), p.k[n - 1].view(torch.uint8)) and torch.equal(p.v[61].view(torch.uint8), p.v[int(tables[0][0][0])].view(torch.uint8))
+
+
+def test_refusals_of_the_binding():
+    p = tq.make_pages(4, 2, 64, 16, device=DEV)
+    table, lens = ints([[0, 1]]), ints([5])
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device=DEV)
+    kv = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device=DEV)
+    ok = (table, lens, None, 1, 0.1)
+    tq.tq_pages_attend(p, q, *ok, torch.empty_like(q))
+    for match, f in [
+            ("dtype", lambda: tq.tq_pages_attend(p, q.half(), *ok, q.half())),
+            ("out", lambda: tq.tq_pages_attend(p, q, *ok, q.float())),
+            ("out", lambda: tq.tq_pages_attend(p, q, *ok, q[:, :2])),
+            ("overlap", lambda: tq.tq_pages_attend(p, q, *ok, q[:, :1].expand(1, 4, 64))),
+            ("expected", lambda: tq.tq_pages_attend(p, q[:, :, :32], *ok, q[:, :, :32])),
+            ("heads", lambda: tq.tq_pages_attend(p, q[:, :3], *ok, q[:, :3])),
+            ("UNSUPPORTED", lambda: tq.tq_pages_attend(p, torch.zeros(300, dtype=torch.bfloat16, device=DEV)[4:260].view(1, 4, 64), *ok, q.clone())),
+            ("GPU tensor", lambda: tq.tq_pages_attend(p, q.cpu(), *ok, q)),
+            ("GPU tensor", lambda: tq.tq_pages_attend(p, q, table.cpu(), lens, None, 1, 0.1, q)),
+            ("lens", lambda: tq.tq_pages_attend(p, q, table, lens.long(), None, 1, 0.1, q)),
+            ("lens", lambda: tq.tq_pages_attend(p, q, table, ints([5, 5]), None, 1, 0.1, q)),
+            ("starts", lambda: tq.tq_pages_attend(p, q, table, lens, ints([0]), 1, 0.1, q)),
+            ("table", lambda: tq.tq_pages_attend(p, q, ints([0, 1]), lens, None, 1, 0.1, q)),
+            ("max_new", lambda: tq.tq_pages_attend(p, q, table, lens, None, 2, 0.1, q)),
+            ("lse", lambda: tq.tq_pages_attend(p, q, *ok, q.clone(), lse=torch.zeros(1, 3, device=DEV))),
+            ("chosen", lambda: tq.tq_pages_attend(p, q, *ok, q.clone(), chosen=ints([[[0]]]))),
+            ("INVALID", lambda: tq.tq_pages_attend(p, q, *ok, q.clone(), window=-1)),
+            ("k: 1 heads", lambda: tq.tq_pages_append(p, kv[:, :1], kv[:, :1], table, lens, None, 1)),
+            ("v", lambda: tq.tq_pages_append(p, kv, kv.float(), table, lens, None, 1)),
+            ("strides", lambda: tq.tq_pages_append(p, torch.zeros((2, 2, 64), device=DEV), torch.zeros((2, 4, 64), device=DEV)[:, :2], table, lens, ints([0, 2]), 2)),
+            ("no bounds", lambda: tq.tq_pages_select(p, q, table, lens, None, 1, torch.zeros((1, 2, 2), dtype=torch.int32, device=DEV))),
+            ("parents", lambda: tq.tq_pages_fork(p, table, lens, [0], ints([0]))),
+            ("children", lambda: tq.tq_pages_fork(p, table, lens, ints([0]), ints([0, 1]))),
+            ("missing", lambda: tq.tq_pages_reserve(p, table, lens, 1, missing=ints([0, 0]))),
+            ("dst", lambda: tq.tq_pages_copy(p, ints([0]), ints([0, 1]))),
+            ("reference counts", lambda: tq.tq_pages_free(tq.Pages(p.k, p.v, p.k_scale, p.v_scale), table, lens, ints([0]))),
+            ("k_scale", lambda: tq.Pages(p.k, p.v, p.k_scale[:3], p.v_scale)),
+            ("expected", lambda: tq.Pages(p.k.view(torch.uint8), p.v, p.k_scale, p.v_scale)),
+            ("contiguous", lambda: tq.Pages(p.k[:, :, :, :64].transpose(0, 1).contiguous().transpose(0, 1), p.v, p.k_scale, p.v_scale))]:
+        with pytest.raises(tq.TurboQuantError, match=match):
+            f()
+    # nothing to do
+    none = torch.empty((0, 4, 64), dtype=torch.bfloat16, device=DEV)
+    tq.tq_pages_attend(p, none, ints(np.zeros((0, 2))), ints([]), None, 1, 0.1, none)
+    tq.tq_pages_attend(p, q, table, lens, None, 0, 0.1, q.clone())
+    out = torch.full_like(q, 7.0)
+    tq.tq_pages_attend(p, q, *ok, out, chosen=torch.empty((1, 2, 0), dtype=torch.int32, device=DEV))
+    assert (out == 0).all()
+    tq.tq_pages_free(p, table, lens, ints([]))
+    tq.tq_pages_copy(p, ints([]), ints([]))
+
+
+def test_without_the_compiled_half(monkeypatch):
+    from paper_2504_19874_amd import _lib
+    monkeypatch.setattr(_lib, "_call", _lib._Checked())
+    test_a_serving_run("e4m3")
+    test_views_of_wider_arrays()
+    T.run_attend(1, 128, 64, "e4m3", "bf16", 2, 4, [1, 33, 64], [1, 1, 1])
