@@ -404,24 +404,29 @@ __global__ __launch_bounds__(256) void pages_join_kernel(const PagesAttendArgs a
   const int64_t row = a.b.first_row(s) + t;
   if (row < 0 || row >= a.b.n_rows) return;
   const float* const part = a.part + (row * heads + head) * a.splits * kPart<D>;
-  float m = -INFINITY, l = 0.f;
-  if (lane < a.splits) m = part[lane * kPart<D>], l = part[lane * kPart<D> + 1];
-  const float top = over_wavefront(m, [](float x, float y) { return fmaxf(x, y); });
-  const float f = l == 0.f ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-  const float sum = over_wavefront(f * l, [](float x, float y) { return x + y; });
-  float y[VE] = {};
-  for (int i0 = 0; i0 < a.splits; i0 += 16) {  // 16 loads on their way
-    float x[16][VE];
+  // 16 ranges on their way at a time, the first before anything is waited for
+  float x[16][VE];
+  const auto fetch = [&](int i0) {
 #pragma unroll
     for (int u = 0; u < 16; ++u)
 #pragma unroll
       for (int c = 0; c < VE; ++c) x[u][c] = part[(i0 + u < a.splits ? i0 + u : 0) * kPart<D> + 4 + lane * VE + c];
+  };
+  float m = -INFINITY, l = 0.f;
+  if (lane < a.splits) m = part[lane * kPart<D>], l = part[lane * kPart<D> + 1];
+  fetch(0);
+  const float top = over_wavefront(m, [](float p, float q) { return fmaxf(p, q); });
+  const float f = l == 0.f ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+  const float sum = over_wavefront(f * l, [](float p, float q) { return p + q; });
+  float y[VE] = {};
+  for (int i0 = 0; i0 < a.splits; i0 += 16) {
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
       const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i0 + u));  // (0 behind the last range)
 #pragma unroll
       for (int c = 0; c < VE; ++c) y[c] = fmaf(w, x[u][c], y[c]);
     }
+    if (i0 + 16 < a.splits) fetch(i0 + 16);
   }
   store_row<VE, F32>(a.out, row, head, lane * VE, y, sum);
   if (a.lse != nullptr && lane == 0) a.lse[row * heads + head] = log_sum(top, sum);

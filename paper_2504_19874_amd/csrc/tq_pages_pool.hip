@@ -203,27 +203,31 @@ __global__ __launch_bounds__(THREADS) void pages_compact_kernel(const PagesView 
     plan[1] = live;
     if (n_live != nullptr) *n_live = live;
   }
+  __syncthreads();
+  for (int i = threadIdx.x; i < moves; i += THREADS) at[move[2 * i]] = move[2 * i + 1];
 }
 
-__global__ __launch_bounds__(256) void pages_move_kernel(const PagesView c, const int32_t* plan, const int32_t* move, int32_t* at, const int d) {
-  const int moves = plan[0], piece = blockIdx.y;
+// the table's rows (blockIdx.y 0), and the pieces of the pages that move
+__global__ __launch_bounds__(256) void pages_move_kernel(const PagesView c, const BatchView b, const int32_t* plan, const int32_t* move,
+                                                        const int32_t* at, const int d) {
+  const int moves = plan[0], live = plan[1], piece = (int)blockIdx.y - 1;
+  if (piece < 0) {  // the table
+    for (int s = blockIdx.x; s < b.n_seqs; s += gridDim.x) {
+      int32_t* const row = b.table + (int64_t)s * b.table_stride;
+      for (int j = threadIdx.x; j < b.width; j += 256) {
+        const int p = row[j];
+        if (p >= live && p < c.n_pages) row[j] = at[p];
+      }
+    }
+    return;
+  }
   for (int i = blockIdx.x; i < moves; i += gridDim.x) {
     const int from = move[2 * i], to = move[2 * i + 1];
     if (piece == 0 && threadIdx.x == 0) {
-      at[from] = to;
       c.refs[to] = c.refs[from];
       c.refs[from] = 0;
     }
     copy_piece(c, d, from, to, piece);
-  }
-}
-
-__global__ __launch_bounds__(256) void pages_retable_kernel(const PagesView c, const BatchView b, const int32_t* plan, const int32_t* at) {
-  const int live = plan[1];
-  int32_t* const row = b.table + (int64_t)blockIdx.x * b.table_stride;
-  for (int j = blockIdx.y * 256 + threadIdx.x; j < b.width; j += gridDim.y * 256) {
-    const int p = row[j];
-    if (p >= live && p < c.n_pages) row[j] = at[p];
   }
 }
 
@@ -267,15 +271,10 @@ hipError_t launch_pages_compact(const PagesView& c, const BatchView& b, int d, i
   hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(THREADS), 0, s, c, plan, move, at, n_live);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (c.n_pages > 1) {
-    const dim3 grid((unsigned)(c.n_pages / 2 < 2048 ? c.n_pages / 2 : 2048), (unsigned)pieces_of(c, d));
-    hipLaunchKernelGGL(pages_move_kernel, grid, dim3(256), 0, s, c, plan, move, at, d);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (b.n_seqs > 0 && b.width > 0) {
-    const int spans = (b.width + 1023) / 1024;
-    hipLaunchKernelGGL(pages_retable_kernel, dim3((unsigned)b.n_seqs, (unsigned)(spans < 64 ? spans : 64)), dim3(256), 0, s, c, b, plan, at);
+  const int64_t pairs = c.n_pages / 2 > b.n_seqs ? c.n_pages / 2 : b.n_seqs;
+  if (pairs > 0) {
+    const dim3 grid((unsigned)(pairs < 2048 ? pairs : 2048), (unsigned)pieces_of(c, d) + 1);
+    hipLaunchKernelGGL(pages_move_kernel, grid, dim3(256), 0, s, c, b, plan, move, at, d);
     e = hipGetLastError();
   }
   return e;
