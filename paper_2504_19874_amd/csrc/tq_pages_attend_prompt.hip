@@ -174,20 +174,25 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   const auto step = [&](int half, const int (&sp)[4], const float (&ks)[4], const float (&lv)[4], const float (&iv)[4], bool masked) {
     const uint4_t* const keys = lds + 2 * half * TILE;
     const uint4_t* const values = keys + TILE;
+    // Fragments are fetched a phase ahead of their products (a product takes 32 cycles, a fetch over 100), and the barriers keep them there
+    uint4_t kf[KS], vf[2 * DT];
+    const auto fetch_keys = [&](int kt) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[k] = keys[(kt * KS + k) * 64 + (lane ^ (k & 7))];
+    };
+    fetch_keys(0);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       float16_t acc;
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        union {
-          uint4_t w;
-          bf16x8_t v;
-        } f;
-        f.w = keys[(kt * KS + k) * 64 + (lane ^ (k & 7))];
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, q[k], acc, 0, 0, 0);
-      }
+      for (int k = 0; k < KS; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[k]), q[k], acc, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2 * DT; ++i) vf[i] = values[(2 * kt * DT + i) * 64 + lane];
+      __builtin_amdgcn_sched_barrier(0);
       uint32_t hidden = 0;  // bit i: key 8 (i / 4) + 4 b + i % 4 is not seen
       if (masked) {
         const bool inner = max(sp[2 * kt], sp[2 * kt + 1]) + 15 <= mine_lo && (int64_t)min(sp[2 * kt], sp[2 * kt + 1]) > (int64_t)mine_hi - a.window;
@@ -242,17 +247,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         l = fmaf(w, iv[2 * kt + (i >> 3)], l);
         p[i >> 3][i & 7] = (_Float16)w;
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[t]), p[0], o[t], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (kt == 0) fetch_keys(1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          union {
-            uint4_t w;
-            half8_t v;
-          } f;
-          f.w = values[((2 * kt + u) * DT + t) * 64 + lane];
-          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.v, p[u], o[t], 0, 0, 0);
-        }
+      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[DT + t]), p[1], o[t], 0, 0, 0);
     }
   };
 
