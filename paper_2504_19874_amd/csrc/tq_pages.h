@@ -84,13 +84,14 @@ struct PagesAttendArgs {
   int window;  // of tokens that a row sees; INT_MAX: all
   int splits;   // ranges that the keys of a unit are cut into
   bool prompt;  // the kernel for prompts
+  int tiles;    // of 16 rows to a workgroup of the other kernel
   float* part;  // what they leave, [n_rows][query heads][splits][4 + d]; with one range unused
 };
 // workgroups of one range each: sequences (or rows) times heads times tiles of query rows
-int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen);
+int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen, int tiles);
 struct PagesAttendPlan {
   bool prompt;
-  int splits;
+  int splits, tiles;
 };
 PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits);

@@ -164,7 +164,7 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
   if (!attend_fits(b, c->n_heads, a.group, chosen != nullptr)) return TQ_ERR_UNSUPPORTED;
   PagesAttendPlan plan;
   const size_t need = attend_part_bytes(c, b, dtype == TQ_F32, a.group, chosen != nullptr, n_chosen, window, &plan);
-  a.splits = plan.splits, a.prompt = plan.prompt;
+  a.splits = plan.splits, a.prompt = plan.prompt, a.tiles = plan.tiles;
   if (need > 0 && (c->workspace == nullptr || c->workspace_bytes < need || misaligned(c->workspace))) return TQ_ERR_WORKSPACE;
   a.part = static_cast<float*>(c->workspace);
   return from_hip(launch_pages_attend(c->d, c->type, dtype == TQ_F32, a, static_cast<hipStream_t>(stream)));

@@ -316,79 +316,83 @@ struct Walk {
   }
 };
 
-// One unit and 16 rows to a workgroup, whose wavefronts share the keys of one range.
-template <int D, int CT, bool F32>
+// One unit and 16 R rows to a workgroup, whose wavefronts share the keys of one range.
+template <int D, int CT, bool F32, int R>
 __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAttendArgs a) {
   constexpr int VE = D / 16;
   __shared__ float o_s[2][16][D + 4];
   __shared__ float ml_s[WAVES][16][2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 15) / 16);
+  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 16 * R - 1) / (16 * R));
   const int split = (int)(blockIdx.x % (unsigned)a.splits);
   const unsigned unit = blockIdx.x / (unsigned)a.splits;
   const int tile = (int)(unit % (unsigned)row_tiles);
-  Walk<D, CT, F32, 1> w(a);
-  if (!w.start(unit / (unsigned)row_tiles, 16 * tile)) return;
+  Walk<D, CT, F32, R> w(a);
+  if (!w.start(unit / (unsigned)row_tiles, 16 * R * tile)) return;
   // this wavefront's tiles: an equal part of them, in one piece
   const int tiles = w.tiles(), each = (tiles + a.splits * WAVES - 1) / (a.splits * WAVES);
   const int begin = (split * WAVES + wave) * each;
   w.run(begin, min(begin + each, tiles));
   const int r = w.r, g = w.g, heads = w.heads, group = a.group;
-  const float M = w.M[0], l = swap_sum(w.l[0]);
+#pragma unroll
+  for (int i16 = 0; i16 < R; ++i16) {
+    if (i16 > 0) __syncthreads();  // the sums of the 16 rows before are still read
+    const float M = w.M[i16], l = swap_sum(w.l[i16]);
 
-  // The wavefronts' sums in one frame.  Lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
-  if (g == 0) ml_s[wave][r][0] = M, ml_s[wave][r][1] = l;
-  __syncthreads();
-  float top = ml_s[0][r][0];
-#pragma unroll
-  for (int i = 1; i < WAVES; ++i) top = fmaxf(top, ml_s[i][r][0]);
-  const float down = M == -INFINITY && l == 0.f ? 0.f : M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
-  float* const mine_s = &o_s[wave & 1][r][g * (D / 4)];
-  for (int pair = 0; pair < WAVES; pair += 2) {
-    if ((wave & ~1) == pair) {
-#pragma unroll
-      for (int c = 0; c < D / 4; c += 4) {
-        float4_t y = {};
-        if (pair != 0) y = *reinterpret_cast<const float4_t*>(mine_s + c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += w.o[0][(c + i) % VE][(c + i) / VE] * down;
-        *reinterpret_cast<float4_t*>(mine_s + c) = y;
-      }
-    }
+    // The wavefronts' sums in one frame.  Lane (r, g): row r, coordinates [g d / 4, (g + 1) d / 4): o[e][i] is coordinate g d / 4 + i d / 16 + e
+    if (g == 0) ml_s[wave][r][0] = M, ml_s[wave][r][1] = l;
     __syncthreads();
-  }
+    float top = ml_s[0][r][0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, ml_s[i][r][0]);
+    const float down = M == -INFINITY && l == 0.f ? 0.f : M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+    float* const mine_s = &o_s[wave & 1][r][g * (D / 4)];
+    for (int pair = 0; pair < WAVES; pair += 2) {
+      if ((wave & ~1) == pair) {
+#pragma unroll
+        for (int c = 0; c < D / 4; c += 4) {
+          float4_t y = {};
+          if (pair != 0) y = *reinterpret_cast<const float4_t*>(mine_s + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] += w.o[i16][(c + i) % VE][(c + i) / VE] * down;
+          *reinterpret_cast<float4_t*>(mine_s + c) = y;
+        }
+      }
+      __syncthreads();
+    }
 
-  // thread: one row, D / 16 coordinates of it
-  const int out_r = threadIdx.x >> 4, first = (threadIdx.x & 15) * VE;
-  const int m2 = tile * 16 + out_r;
-  if (m2 >= w.rows) return;
-  const int64_t row2 = w.row_of(m2);
-  const int head2 = w.head_of(m2);
-  if (row2 < 0 || row2 >= a.b.n_rows) return;
-  float m = ml_s[0][out_r][0], sum = 0.f;
+    // thread: one row, D / 16 coordinates of it
+    const int out_r = threadIdx.x >> 4, first = (threadIdx.x & 15) * VE;
+    const int m2 = (tile * R + i16) * 16 + out_r;
+    if (m2 >= w.rows) continue;
+    const int64_t row2 = w.row_of(m2);
+    const int head2 = w.head_of(m2);
+    if (row2 < 0 || row2 >= a.b.n_rows) continue;
+    float m = ml_s[0][out_r][0], sum = 0.f;
 #pragma unroll
-  for (int i = 1; i < WAVES; ++i) m = fmaxf(m, ml_s[i][out_r][0]);
+    for (int i = 1; i < WAVES; ++i) m = fmaxf(m, ml_s[i][out_r][0]);
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    const float mw = ml_s[i][out_r][0], lw = ml_s[i][out_r][1];
-    sum += lw == 0.f ? 0.f : mw == m ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
+    for (int i = 0; i < WAVES; ++i) {
+      const float mw = ml_s[i][out_r][0], lw = ml_s[i][out_r][1];
+      sum += lw == 0.f ? 0.f : mw == m ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
+    }
+    float y[VE];
+#pragma unroll
+    for (int c = 0; c < VE; c += 4) {
+      const float4_t u = *reinterpret_cast<const float4_t*>(&o_s[0][out_r][first + c]), v = *reinterpret_cast<const float4_t*>(&o_s[1][out_r][first + c]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[c + i] = u[i] + v[i];
+    }
+    if (a.splits > 1) {
+      float* const part = a.part + ((row2 * heads * group + head2) * a.splits + split) * kPart<D>;
+#pragma unroll
+      for (int c = 0; c < VE; c += 4) *reinterpret_cast<float4_t*>(part + 4 + first + c) = float4_t{y[c], y[c + 1], y[c + 2], y[c + 3]};
+      if (first == 0) part[0] = m, part[1] = sum;
+      continue;
+    }
+    store_row<VE, F32>(a.out, row2, head2, first, y, sum);
+    if (a.lse != nullptr && first == 0) a.lse[row2 * heads * group + head2] = log_sum(m, sum);
   }
-  float y[VE];
-#pragma unroll
-  for (int c = 0; c < VE; c += 4) {
-    const float4_t u = *reinterpret_cast<const float4_t*>(&o_s[0][out_r][first + c]), v = *reinterpret_cast<const float4_t*>(&o_s[1][out_r][first + c]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[c + i] = u[i] + v[i];
-  }
-  if (a.splits > 1) {
-    float* const part = a.part + ((row2 * heads * group + head2) * a.splits + split) * kPart<D>;
-#pragma unroll
-    for (int c = 0; c < VE; c += 4) *reinterpret_cast<float4_t*>(part + 4 + first + c) = float4_t{y[c], y[c + 1], y[c + 2], y[c + 3]};
-    if (first == 0) part[0] = m, part[1] = sum;
-    return;
-  }
-  store_row<VE, F32>(a.out, row2, head2, first, y, sum);
-  if (a.lse != nullptr && first == 0) a.lse[row2 * heads * group + head2] = log_sum(m, sum);
 }
 
 // one wavefront for each row and head: the ranges of keys in one frame
@@ -438,9 +442,13 @@ hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
   if (a.prompt) {
     e = launch_pages_attend_prompt(D, CT, a, s);
   } else {
-    const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr) * a.splits));
-    if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true>), grid, dim3(64 * WAVES), 0, s, a);
-    else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false>), grid, dim3(64 * WAVES), 0, s, a);
+    const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr, a.tiles) * a.splits));
+    if (a.tiles == 2) {
+      if constexpr (D == 128) hipLaunchKernelGGL((pages_attend_kernel<D, CT, false, 2>), grid, dim3(64 * WAVES), 0, s, a);
+    } else {
+      if (f32) hipLaunchKernelGGL((pages_attend_kernel<D, CT, true, 1>), grid, dim3(64 * WAVES), 0, s, a);
+      else hipLaunchKernelGGL((pages_attend_kernel<D, CT, false, 1>), grid, dim3(64 * WAVES), 0, s, a);
+    }
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.splits == 1) return e;
@@ -452,20 +460,25 @@ hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen) {
+int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen, int tiles) {
   const int64_t rows = (chosen ? 1 : (int64_t)b.max_new) * group;
-  return (int64_t)b.n_seqs * heads * (chosen ? b.max_new : 1) * ((rows + 15) / 16);
+  return (int64_t)b.n_seqs * heads * (chosen ? b.max_new : 1) * ((rows + 16 * tiles - 1) / (16 * tiles));
 }
 
 PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window) {
   int64_t keys = (int64_t)(chosen ? n_chosen : b.width) << log2_page;
   if (!chosen && window + b.max_new < keys) keys = window + b.max_new;
-  const int64_t units = pages_attend_units(b, heads, group, chosen), rows = (int64_t)b.max_new * group;
-  PagesAttendPlan plan = {false, 1};
+  const int64_t rows = (chosen ? 1 : (int64_t)b.max_new) * group;
+  PagesAttendPlan plan = {false, 1, 1};
+  // More than 16 rows of bf16 queries, d = 128, and keys enough for every compute unit: 32 rows to a workgroup, which fetches and turns a tile
+  // once for them.  us with 16 / 32 rows, 8 x 4 heads after 4096 tokens: 64 sequences of 8 rows 154 / 121, of 16 288 / 205, eight of 8
+  // 30.1 / 25.6, one 12.9 / 14.3, one after 60000 37.0 / 34.3.  (d = 64: 27.0 / 27.3 for 16 sequences of 8 rows)
+  if (rows > 16 && !f32 && d == 128 && pages_attend_units(b, heads, group, chosen, 1) * keys >= 2048ll * device_cu_count()) plan.tiles = 2;
+  const int64_t units = pages_attend_units(b, heads, group, chosen, plan.tiles);
   if (units == 0) return plan;
   // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys until every compute unit has a workgroup.
   // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 991 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
-  // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 155, 16 (64 rows) 263 / 292, 32 279 / 577
+  // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577
   const int64_t blocks = (int64_t)b.n_seqs * heads * ((rows + 255) / 256);
   if (!chosen && !f32 && d != 256 && rows > 64) {
     const int64_t fill = (device_cu_count() + blocks - 1) / blocks, most = (keys + 1023) / 1024;

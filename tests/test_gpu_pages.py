@@ -190,6 +190,14 @@ def test_prompts(case):
     run_attend(8, d, page, kind, "bf16", heads, group, lens, new, window)
 
 
+@pytest.mark.parametrize("kind,group,new,chosen", [("e4m3", 4, 5, 0), ("int8", 3, 11, 0), ("e4m3", 20, 2, 40)])
+def test_more_than_16_rows_of_many_sequences(kind, group, new, chosen):
+    """32 rows to a workgroup."""
+    n = 40 if chosen else 64
+    lens = [7 + 9 * i for i in range(n - 1)] + [600]
+    run_attend(9, 128, 16, kind, "bf16", 8, group, lens, [min(new, m) for m in lens], chosen=chosen or None)
+
+
 @pytest.mark.parametrize("d,dtype,seqs,new", [(128, "bf16", 1, 7), (64, "f32", 1, 20), (128, "bf16", 20, 70), (64, "bf16", 20, 70)])
 def test_what_a_row_does_not_see_does_not_reach_it(d, dtype, seqs, new):
     """NaN among later tokens' keys and values, in what a window has left behind, and behind the last token: rows that see none of it have
