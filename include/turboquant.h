@@ -588,9 +588,9 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  * and not there (their entries stay -1).  Results do not depend on any order of execution.  n_pages <= 2^22 for these calls.
  *   tq_pages_reserve  every entry that is no page among those that hold the last max_new positions below lens[s] gets a
  *                     free page (refs = 1): to be called before an append, with lens already counting the new tokens.
- *   tq_pages_fork     row children[i] (which holds no pages) becomes a copy of row parents[i]: full pages are shared
- *                     (refs + 1), a last page that is not full is copied into a free one.  Children are distinct rows and
- *                     no parents; a row outside [0, n_seqs) is skipped.
+ *   tq_pages_fork     row children[i] (lens 0, holding no pages) becomes a copy of row parents[i]: full pages are shared
+ *                     (refs + 1), a last page that is not full is copied into a free one.  Skipped are a row outside
+ *                     [0, n_seqs), a child that holds tokens (its parent itself too) or that an earlier entry has.
  *   tq_pages_free     rows rows[i] give back what they hold (refs - 1): their entries become -1, their lens 0.
  *   tq_pages_compact  the pages in use move to [0, n_live): those at n_live and above, in order, into the free pages below,
  *                     in order.  Contents, refs and the batch's table follow; n_live: device, nullable.  Every table row

@@ -161,9 +161,15 @@ class Pool:
 
     def fork(self, parents, children):
         moves, missing = [], 0
-        fresh = {}
+        fresh, taken = {}, set()
+        skip = []
+        for p, c in zip(parents, children):
+            skip.append(not (0 <= p < len(self.lens) and 0 <= c < len(self.lens)) or p == c or self.lens[c] > 0 or c in taken)
+            if not skip[-1]:
+                taken.add(c)
+        before = self.lens.copy()
         for n, (p, c) in enumerate(zip(parents, children)):  # pages are given out before any count changes
-            if not (0 <= p < len(self.lens) and 0 <= c < len(self.lens)):
+            if skip[n]:
                 continue
             full = self.lens[p] // self.page
             if self.lens[p] % self.page and full < self.table.shape[1] and 0 <= self.table[p, full] < len(self.refs):
@@ -172,9 +178,9 @@ class Pool:
                 if fresh[n] >= 0:
                     moves.append((int(self.table[p, full]), fresh[n]))
         for n, (p, c) in enumerate(zip(parents, children)):
-            if not (0 <= p < len(self.lens) and 0 <= c < len(self.lens)):
+            if skip[n]:
                 continue
-            full = min(self.lens[p] // self.page, self.table.shape[1])
+            full = min(before[p] // self.page, self.table.shape[1])
             self.table[c] = -1
             self.table[c, :full] = self.table[p, :full]
             for x in self.table[c, :full]:
@@ -182,7 +188,7 @@ class Pool:
                     self.refs[x] += 1
             if full < self.table.shape[1]:
                 self.table[c, full] = fresh.get(n, -1)
-            self.lens[c] = self.lens[p]
+            self.lens[c] = before[p]
         return moves, missing
 
     def free(self, rows):

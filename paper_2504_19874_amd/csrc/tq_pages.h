@@ -114,7 +114,7 @@ hipError_t launch_pages_select(int d, bool f32, const PagesSelectArgs& a, hipStr
 
 hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t* list, int32_t* missing, hipStream_t s);
 hipError_t launch_pages_fork(const PagesView& c, const BatchView& b, int d, const int32_t* parents, const int32_t* children, int n, int32_t* list,
-                             int32_t* fresh, int32_t* missing, hipStream_t s);
+                             int32_t* pairs, int32_t* missing, hipStream_t s);  // pairs: 2 n, 8-byte aligned
 hipError_t launch_pages_free(const PagesView& c, const BatchView& b, const int32_t* rows, int n, hipStream_t s);
 hipError_t launch_pages_compact(const PagesView& c, const BatchView& b, int d, int32_t* plan, int32_t* move, int32_t* at, int32_t* n_live, hipStream_t s);
 hipError_t launch_pages_copy(const PagesView& c, int d, const int32_t* src, const int32_t* dst, int64_t n, hipStream_t s);

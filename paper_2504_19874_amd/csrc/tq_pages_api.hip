@@ -90,7 +90,7 @@ size_t attend_part_bytes(const tq_pages* c, const tq_batch* b, bool f32, int gro
   return pages_attend_part_bytes(c->d, v, c->n_heads, group, n.splits);
 }
 
-size_t pool_bytes(const tq_pages* c, int64_t n) { return (size_t)(3 * c->n_pages + n + 64) * sizeof(int32_t); }
+size_t pool_bytes(const tq_pages* c, int64_t n) { return (size_t)(3 * c->n_pages + 2 * n + 64) * sizeof(int32_t); }
 
 tq_status check_pool(const tq_pages* c, const tq_batch* b, int64_t n) {
   tq_status st = check_pages(c);
@@ -217,7 +217,7 @@ tq_status tq_pages_fork(const tq_pages* c, const tq_batch* b, const int32_t* par
   if (st != TQ_OK) return st;
   if (n > 0 && (parents == nullptr || children == nullptr || !batch_arrays(b))) return TQ_ERR_INVALID_ARG;
   int32_t* const list = static_cast<int32_t*>(c->workspace);
-  return from_hip(launch_pages_fork(view(c), view(b), c->d, parents, children, n, list, list + c->n_pages, missing, static_cast<hipStream_t>(stream)));
+  return from_hip(launch_pages_fork(view(c), view(b), c->d, parents, children, n, list, list + (c->n_pages + 1) / 2 * 2, missing, static_cast<hipStream_t>(stream)));
 }
 
 tq_status tq_pages_free(const tq_pages* c, const tq_batch* b, const int32_t* rows, int32_t n, void* stream) {

@@ -71,30 +71,34 @@ __global__ __launch_bounds__(THREADS) void pages_reserve_kernel(const PagesView 
   if (threadIdx.x == 0 && missing != nullptr) *missing = want - got;
 }
 
-// which row is forked into which, and the page of its last tokens if that is not full
+// What fork i does, written by the first kernel for the second: the tokens of its parent (-1: it is skipped) and the free page that the
+// last of them are copied into (-1: none).
 struct Fork {
-  int parent, child, full, from;  // from: the page to be copied, or -1
+  int32_t len, fresh;
 };
-__device__ __forceinline__ bool fork_of(const PagesView& c, const BatchView& b, const int32_t* parents, const int32_t* children, int i, Fork& f) {
-  f.parent = parents[i], f.child = children[i];
-  if (f.parent < 0 || f.parent >= b.n_seqs || f.child < 0 || f.child >= b.n_seqs) return false;
-  const int len = max(b.lens[f.parent], 0);
-  f.full = min(len >> c.log2_page, b.width);
-  f.from = -1;
-  if (f.full < b.width && (len & ((1 << c.log2_page) - 1)) != 0) {
-    const int p = b.table[(int64_t)f.parent * b.table_stride + f.full];
-    if (is_page(c, p)) f.from = p;
-  }
-  return true;
-}
 
-// fresh[i]: the page that fork i copies its last tokens into, or -1
 __global__ __launch_bounds__(THREADS) void pages_fork_kernel(const PagesView c, const BatchView b, const int32_t* parents, const int32_t* children,
-                                                            const int n, int32_t* list, int32_t* fresh, int32_t* missing) {
+                                                            const int n, int32_t* list, Fork* forks, int32_t* missing) {
   __shared__ int wave_s[WAVES];
+  const auto is_row = [&](int s) { return s >= 0 && s < b.n_seqs; };
+  // Of the entries with one child the first counts: i - n, below every length, in the child's place.  A child that holds tokens is left alone.
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    const int p = parents[i], s = children[i];
+    forks[i] = Fork{-1, -1};
+    if (is_row(p) && is_row(s) && p != s && b.lens[s] <= 0) forks[i].len = max(b.lens[p], 0);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += THREADS)
+    if (forks[i].len >= 0) atomicMin(&b.lens[children[i]], i - n);
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += THREADS)
+    if (forks[i].len >= 0 && b.lens[children[i]] != i - n) forks[i].len = -1;
+  __syncthreads();
+  // the page of a parent's last tokens, if that is not full
   const auto wants = [&](int i) {
-    Fork f;
-    return i < n && fork_of(c, b, parents, children, i, f) && f.from >= 0;
+    if (i >= n || forks[i].len < 0) return false;
+    const int full = forks[i].len >> c.log2_page;
+    return (forks[i].len & ((1 << c.log2_page) - 1)) != 0 && full < b.width && is_page(c, b.table[(int64_t)parents[i] * b.table_stride + full]);
   };
   int want = 0;
   for (int i = 0; i < n; i += THREADS) rank_of(wants(i + (int)threadIdx.x), want, wave_s);
@@ -104,10 +108,9 @@ __global__ __launch_bounds__(THREADS) void pages_fork_kernel(const PagesView c, 
     const int i = i0 + (int)threadIdx.x;
     const bool is = wants(i);
     const int rank = rank_of(is, at, wave_s);
-    if (i < n) {
-      const int p = is && rank < got ? list[rank] : -1;
-      fresh[i] = p;
-      if (p >= 0) c.refs[p] = 1;
+    if (is && rank < got) {
+      forks[i].fresh = list[rank];
+      c.refs[list[rank]] = 1;
     }
   }
   if (threadIdx.x == 0 && missing != nullptr) *missing = want - got;
@@ -139,29 +142,30 @@ __device__ __forceinline__ void copy_piece(const PagesView& c, int d, int from, 
   }
 }
 
-// fork i: its table row, the counts of the pages that it shares (piece 0), and its last page's content
+// fork i: its table row, the counts of the pages that it shares (blockIdx.y 0), and its last page's content
 __global__ __launch_bounds__(256) void pages_fork_rows_kernel(const PagesView c, const BatchView b, const int32_t* parents, const int32_t* children,
-                                                             const int32_t* fresh, const int d) {
+                                                             const Fork* forks, const int d) {
   const int i = blockIdx.x, piece = (int)blockIdx.y - 1;
-  Fork f;
-  if (!fork_of(c, b, parents, children, i, f)) return;
+  const Fork f = forks[i];
+  if (f.len < 0) return;
+  const int32_t* const src = b.table + (int64_t)parents[i] * b.table_stride;
+  const int full = min(f.len >> c.log2_page, b.width);
   if (piece >= 0) {
-    if (fresh[i] >= 0) copy_piece(c, d, f.from, fresh[i], piece);
+    if (f.fresh >= 0) copy_piece(c, d, src[full], f.fresh, piece);
     return;
   }
-  const int32_t* const src = b.table + (int64_t)f.parent * b.table_stride;
-  int32_t* const dst = b.table + (int64_t)f.child * b.table_stride;
+  int32_t* const dst = b.table + (int64_t)children[i] * b.table_stride;
   for (int j = threadIdx.x; j < b.width; j += 256) {
     int p = -1;
-    if (j < f.full) {
+    if (j < full) {
       p = src[j];
       if (is_page(c, p)) atomicAdd(&c.refs[p], 1);
-    } else if (j == f.full) {
-      p = fresh[i];
+    } else if (j == full) {
+      p = f.fresh;
     }
     dst[j] = p;
   }
-  if (threadIdx.x == 0) b.lens[f.child] = b.lens[f.parent];
+  if (threadIdx.x == 0) b.lens[children[i]] = f.len;
 }
 
 __global__ __launch_bounds__(256) void pages_free_kernel(const PagesView c, const BatchView b, const int32_t* rows) {
@@ -253,12 +257,13 @@ hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t*
 }
 
 hipError_t launch_pages_fork(const PagesView& c, const BatchView& b, int d, const int32_t* parents, const int32_t* children, int n, int32_t* list,
-                             int32_t* fresh, int32_t* missing, hipStream_t s) {
-  hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(THREADS), 0, s, c, b, parents, children, n, list, fresh, missing);
+                             int32_t* pairs, int32_t* missing, hipStream_t s) {
+  Fork* const forks = reinterpret_cast<Fork*>(pairs);
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(THREADS), 0, s, c, b, parents, children, n, list, forks, missing);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 0) return e;
   const dim3 grid((unsigned)n, (unsigned)pieces_of(c, d) + 1);
-  hipLaunchKernelGGL(pages_fork_rows_kernel, grid, dim3(256), 0, s, c, b, parents, children, fresh, d);
+  hipLaunchKernelGGL(pages_fork_rows_kernel, grid, dim3(256), 0, s, c, b, parents, children, forks, d);
   return hipGetLastError();
 }
 

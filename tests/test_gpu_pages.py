@@ -432,3 +432,51 @@ def test_pool(n_pages, rows, width, page):
     src, dst = [0, 1, n_pages, 2], [n_pages - 1, n_pages - 2, 4, -1]
     tq.tq_pages_copy(p, ints(src), ints(dst))
     assert all(torch.equal(a, b) for a, b in zip(contents(p), moved(got, list(zip(src, dst))[:2])))
+
+
+def test_forks_that_are_skipped():
+    """Rows that are none, a child twice, a child with tokens, a row into itself, an empty parent that is a child as well."""
+    rng = np.random.default_rng(33)
+    p, pool = pool_state(rng, 60, 9, 5, 16, live=4)
+    pool.lens[:4] = [40, 33, 80, 1]
+    pool.table[:], pool.refs[:] = -1, 0
+    for r in range(4):
+        pool.table[r, :-(-pool.lens[r] // 16)] = np.arange(12 * r, 12 * r + -(-pool.lens[r] // 16))
+    pool.refs[pool.table[pool.table >= 0]] = 1
+    p.refs.copy_(ints(pool.refs))
+    table, lens = ints(pool.table), ints(pool.lens)
+    parents = [0, 1, 2, 9, -1, 0, 3, 2, 4, 5, 1, 3]
+    children = [4, 4, 5, 6, 6, -2, 3, 1, 6, 7, 9, 4]
+    want = contents(p)
+    pairs, short = pool.fork(parents, children)
+    missing = ints([-1])
+    tq.tq_pages_fork(p, table, lens, ints(parents), ints(children), missing=missing)
+    assert same_pool(p, pool, table, lens) and int(missing) == short
+    assert all(torch.equal(a, b) for a, b in zip(contents(p), moved(want, pairs)))
+    assert pool.lens.tolist() == [40, 33, 80, 1, 40, 80, 0, 0, 0]
+
+
+def test_many_forks_in_a_pool_that_runs_out():
+    rng = np.random.default_rng(34)
+    p, pool = pool_state(rng, 2100, 3003, 4, 16, heads=1, live=3)
+    pool.lens[:3] = [17, 40, 15]
+    pool.table[:], pool.refs[:] = -1, 0
+    pool.table[0, :2], pool.table[1, :3], pool.table[2, :1] = [5, 7], [2099, 2000, 1], [1024]
+    pool.refs[[5, 7, 2099, 2000, 1, 1024]] = 1
+    p.refs.copy_(ints(pool.refs))
+    table, lens = ints(pool.table), ints(pool.lens)
+    parents, children = rng.integers(0, 3, 3000), 3 + rng.permutation(3000)
+    want = contents(p)
+    pairs, short = pool.fork(parents, children)
+    missing = ints([-1])
+    tq.tq_pages_fork(p, table, lens, ints(parents), ints(children), missing=missing)
+    assert short > 0 and same_pool(p, pool, table, lens) and int(missing) == short
+    assert all(torch.equal(a, b) for a, b in zip(contents(p), moved(want, pairs)))
+    gone = rng.permutation(3003)[:2000]
+    pool.free(gone)
+    tq.tq_pages_free(p, table, lens, ints(gone))
+    want = contents(p)
+    pairs, live = pool.compact()
+    tq.tq_pages_compact(p, table)
+    assert same_pool(p, pool, table, lens)
+    assert all(torch.equal(a, b) for a, b in zip(contents(p), moved(want, pairs)))
