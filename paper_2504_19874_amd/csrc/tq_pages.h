@@ -96,7 +96,7 @@ struct PagesAttendPlan {
 PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits);
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
-// many rows of bf16 queries, d = 64 or 128 (tq_pages_attend_prompt.hip)
+// many rows of bf16 queries (tq_pages_attend_prompt.hip)
 hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s);
 
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,

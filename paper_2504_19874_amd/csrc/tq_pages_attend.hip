@@ -476,14 +476,16 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   if (rows > 16 && !f32 && d == 128 && pages_attend_units(b, heads, group, chosen, 1) * keys >= 2048ll * device_cu_count()) plan.tiles = 2;
   const int64_t units = pages_attend_units(b, heads, group, chosen, plan.tiles);
   if (units == 0) return plan;
-  // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys until every compute unit has a workgroup.
-  // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 991 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
-  // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577
-  const int64_t blocks = (int64_t)b.n_seqs * heads * ((rows + 255) / 256);
-  if (!chosen && !f32 && d != 256 && rows > 64) {
+  // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys until every compute unit has a
+  // workgroup, and taken where half of them (d = 256: three quarters) have one.
+  // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 920 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
+  // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577;
+  // d = 256, where a workgroup has 128 rows: 427 of 1191 129 / 153, 500 of 1000 72 / 64
+  const int64_t block = d == 256 ? 128 : 256, blocks = (int64_t)b.n_seqs * heads * ((rows + block - 1) / block);
+  if (!chosen && !f32 && rows > 64) {
     const int64_t fill = (device_cu_count() + blocks - 1) / blocks, most = (keys + 1023) / 1024;
     plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)16);
-    plan.prompt = 2 * blocks * plan.splits >= device_cu_count();
+    plan.prompt = (d == 256 ? 4 : 6) * blocks * plan.splits >= 3 * device_cu_count();
     if (plan.prompt) return plan;
   }
   // a workgroup for every compute unit, no more ranges than there are tiles for their wavefronts.  One token of 8 x 4 heads after

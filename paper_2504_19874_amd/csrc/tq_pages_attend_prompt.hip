@@ -1,6 +1,6 @@
-// Attention over pages for prompts: many rows of bf16 queries, d = 64 or 128.
+// Attention over pages for prompts: many rows of bf16 queries.
 //
-// The mathematics is that of tq_pages_attend.hip.  Here a workgroup has 256 rows of a sequence and head, 32 to a wavefront, and all
+// The mathematics is that of tq_pages_attend.hip.  Here a workgroup has 256 rows (d = 256: 128) of a sequence and head, 32 to a wavefront, and all
 // wavefronts share one tile of 64 keys in LDS, as 16-bit operands: turning codes into operands (and values by 4 x 4 bytes) is
 // vector work that eight wavefronts would do eight times.  Products on v_mfma_f32_32x32x16, S^T = K Q^T and O^T += V^T P^T:
 // lane (r = lane % 32, b = lane / 32) has row r and of 16 keys 4 b + 0..3 and 8 + 4 b + 0..3 in both, so weights stay in
@@ -8,7 +8,7 @@
 //   keys    [32 keys][16 coordinates][lane]: lane (key, half of the coordinates), its place XOR the coordinates' number, so that eight
 //           lanes that write one key's fragments meet eight groups of banks
 //   values  [16 keys][d tile][lane]: d tile T has the coordinates (d / 32) i + T; a lane fetches d / 32 coordinates of eight keys and
-//           writes a fragment to each d tile (d = 64: four of them, two to each)
+//           writes a fragment to each d tile (d = 64: four coordinates, two to each)
 // Wavefronts 0..3 take the values of one subtile of 16 keys each, 4..7 the keys.  The next tile is fetched while a tile is multiplied
 // and written to the other half of LDS: one barrier a tile.
 #include "tq_pages_attend.h"
@@ -19,12 +19,20 @@ namespace {
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
-constexpr int WAVES = 8, ROWS = 32 * WAVES;
+constexpr int WAVES = 8;
+// d = 256: two wavefronts share 32 rows, each with half of the output's coordinates (and all of S, which is cheaper than its exchange)
+template <int D>
+constexpr int kShare = D == 256 ? 2 : 1;
+template <int D>
+constexpr int kRows = 32 * WAVES / kShare<D>;
 
 template <int D, int CT>
 __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const PagesAttendArgs a) {
   constexpr int KS = D / 16;             // k steps of S
-  constexpr int DT = D / 32;             // d tiles
+  constexpr int ROWS = kRows<D>;
+  constexpr int DA = D / 32, DT = DA / kShare<D>;  // d tiles, and those of a wavefront
+  constexpr int KC = D == 64 ? 4 : D == 128 ? 8 : 4;  // fragments of keys that a lane holds at a time (d = 256: 8 cost 8 % by spills)
+  constexpr int VW = D == 256 ? 2 : 1;   // words of a key's values that a lane turns
   constexpr int KL = D / 64;             // 16-byte loads of a lane's keys
   constexpr int TILE = 64 * D * 2 / 16;  // fragments of a tile's keys, as many of its values
   extern __shared__ uint4_t lds[];       // [2][keys, values][TILE]
@@ -45,13 +53,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   const int64_t row0 = a.b.first_row(s);
   const int at0 = len - whole;
 
-  const int m = min(first + 32 * wave + r, rows - 1);
+  const int rows_of = kShare<D> == 1 ? wave : wave & 3, dh = kShare<D> == 1 ? 0 : wave >> 2;  // which 32 rows, which part of the coordinates
+  const int m = min(first + 32 * rows_of + r, rows - 1);
   const int64_t row = row0 + m / group;
   const int head = h * group + m % group;
-  const bool there = first + 32 * wave + r < rows && row >= 0 && row < a.b.n_rows;
+  const bool there = first + 32 * rows_of + r < rows && row >= 0 && row < a.b.n_rows;
   const int pos = at0 + m / group;
   const int pos_lo = at0 + first / group, pos_hi = at0 + min(first + ROWS - 1, rows - 1) / group;  // of the workgroup
-  const int mine_lo = at0 + min(first + 32 * wave, rows - 1) / group, mine_hi = at0 + min(first + 32 * wave + 31, rows - 1) / group;
+  const int mine_lo = at0 + min(first + 32 * rows_of, rows - 1) / group, mine_hi = at0 + min(first + 32 * rows_of + 31, rows - 1) / group;
 
   bf16x8_t q[KS];
 #pragma unroll
@@ -79,18 +88,25 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     if (at < hi) sub = find_subtile(a.c, table, a.b.width, h, (int)(at >> a.c.log2_page), (int)at & ((1 << a.c.log2_page) - 1));
   };
   // a lane's part of the next tile: wavefronts 0..3 values, 4..7 keys, of subtile wave % 4
-  constexpr int VW = D == 128 ? 1 : 1;  // words of a key's values: four coordinates
   uint32_t raw[8 * VW > 4 * KL ? 8 * VW : 4 * KL];
   const bool has_values = wave < 4;
-  const int dq = D == 128 ? r : r & 15;
+  const int dq = D == 64 ? r & 15 : r;
   const auto fetch = [&](int tile) {
     const int at = __builtin_amdgcn_readlane(sub.at, ((tile & 15) << 2) + (wave & 3));
     const int64_t off = (int64_t)(at < 0 ? 0 : at) * (16 * D);
     if (has_values) {
-      if (D == 128 || r < 16) {
-        const uint8_t* const p = a.c.v + off + 4 * dq;
+      if (D != 64 || r < 16) {
+        const uint8_t* const p = a.c.v + off + 4 * VW * dq;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) raw[j] = *reinterpret_cast<const uint32_t*>(p + (4 * b + (j & 3) + (j >> 2) * 8) * D);
+        for (int j = 0; j < 8; ++j) {
+          const uint8_t* const from = p + (4 * b + (j & 3) + (j >> 2) * 8) * D;
+          if constexpr (VW == 1) {
+            raw[j] = *reinterpret_cast<const uint32_t*>(from);
+          } else {
+            const uint2_t two = *reinterpret_cast<const uint2_t*>(from);
+            raw[j] = two[0], raw[8 + j] = two[1];
+          }
+        }
       }
     } else {
       const uint8_t* const p = a.c.k + off + 16 * lane;  // 16 keys of d bytes in one piece
@@ -105,37 +121,42 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         uint32_t flags = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const uint32_t n = D == 128 || r < 16 ? nan_bytes(raw[j]) : 0u;
-          raw[j] &= ~n;
+          uint32_t n = 0;
+          if (D != 64 || r < 16)
+#pragma unroll
+            for (int v = 0; v < VW; ++v) {
+              const uint32_t bytes = nan_bytes(raw[8 * v + j]);
+              raw[8 * v + j] &= ~bytes;
+              n |= bytes;
+            }
           const uint64_t lanes = __builtin_amdgcn_ballot_w64(n != 0);
           const int key = (j & 3) + (j >> 2) * 8;
           flags |= ((uint32_t)lanes != 0 ? 1u << key : 0u) | ((uint32_t)(lanes >> 32) != 0 ? 16u << key : 0u);
         }
         if (lane == 0) poison_s[half][sb] = (uint16_t)flags;
       }
-      if (D == 128 || r < 16) {
-        uint4_t* const to = lds + (2 * half + 1) * TILE + sb * (DT * 64) + 32 * b;
-        uint32_t turned[2][4];
+      if (D != 64 || r < 16) {
+        uint4_t* const to = lds + (2 * half + 1) * TILE + sb * (DA * 64) + 32 * b;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t w0 = raw[4 * u], w1 = raw[4 * u + 1], w2 = raw[4 * u + 2], w3 = raw[4 * u + 3];
-          const uint32_t a0 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a1 = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
-          const uint32_t b0 = __builtin_amdgcn_perm(w3, w2, 0x05010400u), b1 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
-          turned[u][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
-          turned[u][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
-          turned[u][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
-          turned[u][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
-        }
+        for (int v = 0; v < VW; ++v) {
+          uint32_t turned[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          union {
-            half8_t h;
-            uint4_t w;
-          } f;
-          f.h = codes_fp16<CT>(turned[0][e], turned[1][e]);
-          // coordinate 4 dq + e = (d / 32) i + T
-          if constexpr (D == 128) to[e * 64 + dq] = f.w;
-          else to[(e & 1) * 64 + 2 * dq + (e >> 1)] = f.w;
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t *const w = raw + 8 * v + 4 * u;
+            const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+            const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+            turned[u][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+            turned[u][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+            turned[u][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+            turned[u][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint4_t f = __builtin_bit_cast(uint4_t, codes_fp16<CT>(turned[0][e], turned[1][e]));
+            // coordinate 4 VW dq + 4 v + e = (d / 32) i + T
+            if constexpr (D == 64) to[(e & 1) * 64 + 2 * dq + (e >> 1)] = f;
+            else to[(4 * v + e) * 64 + dq] = f;
+          }
         }
       }
     } else {
@@ -175,12 +196,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     const uint4_t* const keys = lds + 2 * half * TILE;
     const uint4_t* const values = keys + TILE;
     // Fragments are fetched a phase ahead of their products (a product takes 32 cycles, a fetch over 100), and the barriers keep them there
-    uint4_t kf[KS], vf[2 * DT];
-    const auto fetch_keys = [&](int kt) {
+    uint4_t kf[KC], vf[2 * DT];
+    const auto fetch_keys = [&](int kt, int k0) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[k] = keys[(kt * KS + k) * 64 + (lane ^ (k & 7))];
+      for (int k = 0; k < KC; ++k) kf[k] = keys[(kt * KS + k0 + k) * 64 + (lane ^ ((k0 + k) & 7))];
     };
-    fetch_keys(0);
+    fetch_keys(0, 0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -188,10 +209,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[k]), q[k], acc, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int k0 = 0; k0 < KS; k0 += KC) {
+        if (k0 > 0) fetch_keys(kt, k0);
 #pragma unroll
-      for (int i = 0; i < 2 * DT; ++i) vf[i] = values[(2 * kt * DT + i) * 64 + lane];
+        for (int k = 0; k < KC; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[k]), q[k0 + k], acc, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * DT; ++i) vf[i] = values[((2 * kt + i / DT) * DA + dh * DT + i % DT) * 64 + lane];
       __builtin_amdgcn_sched_barrier(0);
       uint32_t hidden = 0;  // bit i: key 8 (i / 4) + 4 b + i % 4 is not seen
       if (masked) {
@@ -251,7 +276,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[t]), p[0], o[t], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
-      if (kt == 0) fetch_keys(1);
+      if (kt == 0) fetch_keys(1, 0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[DT + t]), p[1], o[t], 0, 0, 0);
@@ -289,25 +314,28 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]);
   if (!there) return;
-  // o[t][i] is coordinate (d / 32) (8 (i / 4) + 4 b + i % 4) + t
+  // o[t][i] is coordinate (d / 32) (8 (i / 4) + 4 b + i % 4) + t, of the second part 4 more: in one piece for four i, or for one where
+  // wavefronts share the coordinates
+  constexpr int N = kShare<D> == 1 ? 4 * DT : DT;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    float y[4 * DT];
+  for (int c = 0; c < 16 * DT / N; ++c) {
+    float y[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N / DT; ++i)
 #pragma unroll
-      for (int t = 0; t < DT; ++t) y[i * DT + t] = o[t][4 * c + i];
+      for (int t = 0; t < DT; ++t) y[i * DT + t] = o[t][c * (N / DT) + i];
+    const int i0 = c * (N / DT), at = DA * (8 * (i0 >> 2) + 4 * b + (i0 & 3)) + dh * DT;
     if (a.splits == 1) {
-      store_row<4 * DT, false>(a.out, row, head, DT * (8 * c + 4 * b), y, sum);
+      store_row<N, false>(a.out, row, head, at, y, sum);
     } else {
       float* const part = a.part + ((row * heads * group + head) * a.splits + split) * (4 + D);
 #pragma unroll
-      for (int i = 0; i < 4 * DT; i += 4) *reinterpret_cast<float4_t*>(part + 4 + DT * (8 * c + 4 * b) + i) = float4_t{y[i], y[i + 1], y[i + 2], y[i + 3]};
-      if (c == 0 && b == 0) part[0] = M, part[1] = sum;
+      for (int i = 0; i < N; i += 4) *reinterpret_cast<float4_t*>(part + 4 + at + i) = float4_t{y[i], y[i + 1], y[i + 2], y[i + 3]};
+      if (c == 0 && b == 0 && dh == 0) part[0] = M, part[1] = sum;
     }
   }
   if (a.splits > 1) return;
-  if (a.lse != nullptr && b == 0) a.lse[row * heads * group + head] = log_sum(M, sum);
+  if (a.lse != nullptr && b == 0 && dh == 0) a.lse[row * heads * group + head] = log_sum(M, sum);
 }
 
 template <int D, int CT>
@@ -317,7 +345,7 @@ hipError_t launch(const PagesAttendArgs& a, hipStream_t s) {
   const void* const kernel = reinterpret_cast<const void*>(&pages_attend_prompt_kernel<D, CT>);
   const hipError_t e = raise_lds_limit(limit, kernel, bytes);
   if (e != hipSuccess) return e;
-  const int64_t row_tiles = ((int64_t)a.b.max_new * a.group + ROWS - 1) / ROWS;
+  const int64_t row_tiles = ((int64_t)a.b.max_new * a.group + kRows<D> - 1) / kRows<D>;
   hipLaunchKernelGGL((pages_attend_prompt_kernel<D, CT>), dim3((unsigned)((int64_t)a.b.n_seqs * a.c.heads * row_tiles * a.splits)), dim3(64 * WAVES), bytes, s, a);
   return hipGetLastError();
 }
@@ -325,8 +353,8 @@ hipError_t launch(const PagesAttendArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s) {
-  if (type == kPageI8) return d == 64 ? launch<64, kPageI8>(a, s) : launch<128, kPageI8>(a, s);
-  return d == 64 ? launch<64, kPageE4m3>(a, s) : launch<128, kPageE4m3>(a, s);
+  if (type == kPageI8) return d == 64 ? launch<64, kPageI8>(a, s) : d == 128 ? launch<128, kPageI8>(a, s) : launch<256, kPageI8>(a, s);
+  return d == 64 ? launch<64, kPageE4m3>(a, s) : d == 128 ? launch<128, kPageE4m3>(a, s) : launch<256, kPageE4m3>(a, s);
 }
 
 }  // namespace tq

@@ -181,6 +181,9 @@ PROMPTS = [  # more than 64 rows to a head, half the compute units with a workgr
     (128, 128, "int8", 4, 16, [129] * 2 + [300], [129, 65, 67], 0),
     (128, 64, "e4m3", 8, 1, [4100, 66, 3000, 1], [66, 66, 1, 1], 0),  # keys in ranges
     (64, 64, "e4m3", 8, 1, [4100, 66, 3000, 0], [66, 66, 66, 0], 2500),
+    (256, 32, "e4m3", 8, 1, [70 + 13 * i for i in range(16)], [70 - i for i in range(16)], 0),
+    (256, 16, "int8", 4, 3, [257] * 32, [26 - i % 3 for i in range(32)], 31),
+    (256, 64, "e4m3", 8, 1, [4100, 66, 3000, 1], [66, 66, 1, 1], 0),
 ]
 
 
@@ -198,7 +201,7 @@ def test_more_than_16_rows_of_many_sequences(kind, group, new, chosen):
     run_attend(9, 128, 16, kind, "bf16", 8, group, lens, [min(new, m) for m in lens], chosen=chosen or None)
 
 
-@pytest.mark.parametrize("d,dtype,seqs,new", [(128, "bf16", 1, 7), (64, "f32", 1, 20), (128, "bf16", 20, 70), (64, "bf16", 20, 70)])
+@pytest.mark.parametrize("d,dtype,seqs,new", [(128, "bf16", 1, 7), (64, "f32", 1, 20), (128, "bf16", 20, 70), (64, "bf16", 20, 70), (256, "bf16", 20, 70)])
 def test_what_a_row_does_not_see_does_not_reach_it(d, dtype, seqs, new):
     """NaN among later tokens' keys and values, in what a window has left behind, and behind the last token: rows that see none of it have
     the same bits as without it.  A NaN key makes a row NaN; a NaN value its coordinate, or the row."""
