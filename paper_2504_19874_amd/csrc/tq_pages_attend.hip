@@ -490,7 +490,9 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   }
   // a workgroup for every compute unit, no more ranges than there are tiles for their wavefronts.  One token of 8 x 4 heads after
   // 65536, us by workgroups: 128 43.1, 256 34.1, 512 34.8; four after 64 chosen pages: 16.8, 14.9, 15.2; 64 tokens after up to 8192 each
-  // 125 with 512 or 1024
+  // 125 with 512 or 1024.  Up to six tiles to a wavefront the second launch costs more than it saves (8 x 4 heads, 200 / 512 / 700 tokens in one
+  // range 6.6 / 8.2 / 9.0, in more 10.1 / 9.7 / 9.9)
+  if (keys <= (d == 256 ? 512 : 768)) return plan;
   const int64_t fill = (device_cu_count() + units - 1) / units, most = (keys + 32 * WAVES - 1) / (32 * WAVES);
   plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)64);
   return plan;

@@ -162,6 +162,12 @@ ATTEND = [
     (128, 64, "e4m3", "bf16", 2, 4, [500, 20], [1, 1], 100),
     (64, 64, "int8", "bf16", 1, 4, [200, 64], [65, 1], 1),
     (128, 64, "e4m3", "f32", 2, 4, [2100], [2], 0),
+    # keys in ranges that a second launch joins
+    (64, 16, "int8", "bf16", 2, 4, [1000, 5, 900], [1, 2, 1], 0),
+    (64, 32, "e4m3", "f32", 1, 3, [1500, 31], [7, 1], 0),
+    (128, 32, "int8", "f32", 2, 1, [1300, 0, 1], [1, 0, 1], 700),
+    (256, 16, "e4m3", "bf16", 1, 5, [1200, 800], [4, 1], 0),
+    (256, 64, "int8", "f32", 3, 2, [700], [3], 0),
     # rows at positions below zero
     (128, 16, "e4m3", "bf16", 1, 2, [3, 0], [5, 2], 0),
 ]
@@ -236,7 +242,8 @@ def test_what_a_row_does_not_see_does_not_reach_it(d, dtype, seqs, new):
 
 @pytest.mark.parametrize("d,page,kind,dtype,group,lens,new,n", [
     (128, 64, "e4m3", "bf16", 4, [700, 90], [1, 1], 5), (64, 16, "int8", "f32", 3, [300, 33], [4, 2], 9),
-    (256, 32, "e4m3", "f32", 20, [200], [2], 1), (128, 16, "int8", "bf16", 16, [999], [3], 40)])
+    (256, 32, "e4m3", "f32", 20, [200], [2], 1), (128, 16, "int8", "bf16", 16, [999], [3], 40),
+    (64, 16, "e4m3", "f32", 2, [1500, 60], [2, 1], 64), (256, 64, "int8", "bf16", 3, [2000], [3], 20)])
 def test_attend_over_chosen_pages(d, page, kind, dtype, group, lens, new, n):
     run_attend(2, d, page, kind, dtype, 2, group, lens, new, chosen=n)
 
