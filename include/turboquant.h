@@ -496,7 +496,7 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *   Scales  tq_pages_append makes powers of two: the smallest 2^e with amax / 2^e <= 448 (127), e in [-40, 40], amax over
  *           the block's finite values; larger values (infinities among them) take the largest code, NaN takes NaN (int8: 0).
  *           A power of two lets a block whose scale grows be coded again without a second rounding of what stays
- *           representable.  tq_pages_attend takes any positive scales (2^-126 to 2^125).
+ *           representable.  tq_pages_attend takes any positive scales from 2^-40 to 2^40.
  *   Bounds  (optional) the smallest and largest value of every channel of a page's keys, rounded outward to bf16.
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
@@ -556,6 +556,7 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
  *   chosen   NULL: all tokens.  Else device [n_rows][n_heads][n_chosen]: places in the sequence's table (page i holds
  *            tokens [i * page_tokens, ..)) that the row's query heads read, in any order; entries outside [0, width) are
  *            skipped, one that is there twice counts twice.
+ * Prompts and single tokens in one call share a plan made for the longest; in two calls each has its own.
  * Sums, maxima and weights are fp32.  Codes are exact factors in 16 bits; a bf16 query is one exact factor, an fp32 one
  * three; a softmax weight is taken in fp16 (bf16 output: relative error 2^-11, below the output's own half step 2^-8) or as
  * two fp16 pieces (fp32 output: 2^-22), no closer than 2^-32 of the row's largest weight times value scale.
@@ -589,7 +590,8 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  *   tq_pages_reserve  every entry that is no page among those that hold the last max_new positions below lens[s] gets a
  *                     free page (refs = 1): to be called before an append, with lens already counting the new tokens.
  *   tq_pages_fork     row children[i] (lens 0, holding no pages) becomes a copy of row parents[i]: full pages are shared
- *                     (refs + 1), a last page that is not full is copied into a free one.  Skipped are a row outside
+ *                     (refs + 1), a last page that is not full is copied into a free one.  What is shared is not to
+ *                     be appended to: a sequence is cut back (a smaller lens) no further than the pages of its own.  Skipped are a row outside
  *                     [0, n_seqs), a child that holds tokens (its parent itself too) or that an earlier entry has.
  *   tq_pages_free     rows rows[i] give back what they hold (refs - 1): their entries become -1, their lens 0.
  *   tq_pages_compact  the pages in use move to [0, n_live): those at n_live and above, in order, into the free pages below,

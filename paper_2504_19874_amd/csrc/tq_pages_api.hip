@@ -1,4 +1,5 @@
 // The C ABI of the paged 8-bit cache: checks of arguments, workspaces, launches (include/turboquant.h).
+#include <algorithm>
 #include <climits>
 #include <cstdint>
 
@@ -126,7 +127,7 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
   if (st != TQ_OK) return st;
   st = check_rows(v, dtype, ld_row, ld_head, c->d);
   if (st != TQ_OK) return st;
-  if (!launchable(b->n_seqs, ((int64_t)b->max_new + c->page_tokens - 2) / c->page_tokens + 1, 1)) return TQ_ERR_UNSUPPORTED;
+  if (!launchable(b->n_seqs, std::min<int64_t>(((int64_t)b->max_new + c->page_tokens - 2) / c->page_tokens + 1, b->width), 1)) return TQ_ERR_UNSUPPORTED;
   return from_hip(launch_pages_append(c->d, c->type, dtype == TQ_F32, view(c), view(b), PagesRows{k, ld_row, ld_head}, PagesRows{v, ld_row, ld_head},
                                       static_cast<hipStream_t>(stream)));
 }

@@ -14,8 +14,8 @@
 // With C the base-2 logarithm, lane sums and frames are:  x = log2(e) scale s + log2(v_scale) - M + BASE,  w = 2^x,
 // O = sum w c_v,  l = sum w / v_scale; M is the largest log2(e) scale s + log2(v_scale) so far or up to HEAD below it (a new M costs
 // a pass over O, so it is taken only where a weight would leave fp16's range).  The scale of a value block sits in the exponent of
-// its weights and never costs a product.  With |log2 v_scale| <= 40 a weight that underflows (2^-149 below 2^BASE) is less than
-// 2^-60 of l.
+// its weights and never costs a product.  With |log2 v_scale| <= 40 what a weight that underflows (2^-126, the largest is 2^BASE or
+// more) would add to l is less than 2^-50 of it.
 #include <algorithm>
 
 #include "tq_pages_attend.h"

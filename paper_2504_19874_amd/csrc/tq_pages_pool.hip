@@ -251,7 +251,9 @@ hipError_t launch_pages_copy(const PagesView& c, int d, const int32_t* src, cons
 }
 
 hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t* list, int32_t* missing, hipStream_t s) {
-  const int64_t each = (((int64_t)b.max_new + (1 << c.log2_page) - 2) >> c.log2_page) + 1;
+  // max_new positions lie in no more pages than this, nor in more than a sequence has entries
+  int64_t each = (((int64_t)b.max_new + (1 << c.log2_page) - 2) >> c.log2_page) + 1;
+  each = each < b.width ? each : b.width > 0 ? b.width : 1;
   hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(THREADS), 0, s, c, b, (int)each, list, missing);
   return hipGetLastError();
 }

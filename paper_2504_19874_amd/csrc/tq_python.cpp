@@ -269,14 +269,14 @@ int32_t* ints(const Cache& p, PyObject* o, int64_t n) {
   return static_cast<int32_t*>(t.data_ptr());
 }
 
-// table, lens, starts (or None): a batch of n_rows rows
+// table, lens, starts (or None): a batch of n_rows rows (-1: a call without rows)
 tq_batch batch(const Cache& p, int64_t n_rows, PyObject* table, PyObject* lens, PyObject* starts, int32_t max_new) {
   const at::Tensor& t = there(p, table, at::kInt, 2);
   const int64_t n = t.size(0), width = t.size(1);
   if (n > INT32_MAX || width > INT32_MAX || max_new < 0 || (width > 1 && t.stride(1) != 1) || (n > 1 && t.stride(0) < width)) throw NotPlain{};
-  if (starts == Py_None && n_rows < n * max_new) throw NotPlain{};
+  if (starts == Py_None && n_rows >= 0 && n_rows < n * max_new) throw NotPlain{};
   tq_batch b;
-  b.n_seqs = (int32_t)n, b.max_new = max_new, b.n_rows = n_rows, b.width = (int32_t)width;
+  b.n_seqs = (int32_t)n, b.max_new = max_new, b.n_rows = n_rows < 0 ? 0 : n_rows, b.width = (int32_t)width;
   b.table_stride = n > 1 ? t.stride(0) : width;
   b.table = static_cast<int32_t*>(t.data_ptr());
   b.lens = lens == Py_None ? nullptr : ints(p, lens, n);
@@ -383,7 +383,7 @@ PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 6, [&] {
     const Cache p = cache(a);
     pool(p, 0);
-    const tq_batch b = batch(p, INT32_MAX, a[2], a[3], Py_None, integer32(a[4]));
+    const tq_batch b = batch(p, -1, a[2], a[3], Py_None, integer32(a[4]));
     int32_t* const missing = one(p, a[5]);
     void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_reserve(p.c, &b, missing, s); });
@@ -398,7 +398,7 @@ PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (forks > INT32_MAX) throw NotPlain{};
     pool(p, forks);
     const int32_t *const parents = ints(p, a[4], forks), *const children = ints(p, a[5], forks);
-    const tq_batch b = batch(p, 0, a[2], a[3], Py_None, 0);
+    const tq_batch b = batch(p, -1, a[2], a[3], Py_None, 0);
     int32_t* const missing = one(p, a[6]);
     void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_fork(p.c, &b, parents, children, (int32_t)forks, missing, s); });
@@ -412,7 +412,7 @@ PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t many = there(p, a[4], at::kInt, 1).size(0);
     if (many > INT32_MAX || p.c->refs == nullptr) throw NotPlain{};
     const int32_t* const rows = ints(p, a[4], many);
-    const tq_batch b = batch(p, 0, a[2], a[3], Py_None, 0);
+    const tq_batch b = batch(p, -1, a[2], a[3], Py_None, 0);
     void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_free(p.c, &b, rows, (int32_t)many, s); });
   });
@@ -423,7 +423,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 4, [&] {
     const Cache p = cache(a);
     pool(p, 0);
-    const tq_batch b = batch(p, 0, a[2], Py_None, Py_None, 0);
+    const tq_batch b = batch(p, -1, a[2], Py_None, Py_None, 0);
     int32_t* const live = one(p, a[3]);
     void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_compact(p.c, &b, live, s); });

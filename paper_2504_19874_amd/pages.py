@@ -96,17 +96,18 @@ def _ints(t, what, shape, device):
     return t.data_ptr()
 
 
-def _batch(p: Pages, n_rows: int, table, lens, starts, max_new: int):
+def _batch(p: Pages, n_rows, table, lens, starts, max_new: int):
+    """n_rows None: a call without rows."""
     _where(table, "table")
     if table.dtype != torch.int32 or table.dim() != 2 or (table.numel() and table.shape[1] > 1 and table.stride(1) != 1) or table.device != p.device:
         raise TurboQuantError(f"table: expected int32 [n_seqs][width] with contiguous rows on {p.device}, got {table.dtype} {tuple(table.shape)}")
     n, width = table.shape
     if n > 1 and table.stride(0) < width:
         raise TurboQuantError("table: rows overlap")
-    if max_new < 0 or (starts is None and n_rows < n * max_new):
+    if max_new < 0 or (starts is None and n_rows is not None and n_rows < n * max_new):
         raise TurboQuantError(f"max_new: {n} sequences of {max_new} rows each, and {n_rows} rows")
     b = _lib.TqBatch()
-    b.n_seqs, b.max_new, b.n_rows, b.width = n, max_new, n_rows, width
+    b.n_seqs, b.max_new, b.n_rows, b.width = n, max_new, n_rows or 0, width
     b.table_stride = table.stride(0) if n > 1 else width
     b.table, b.lens = table.data_ptr(), 0 if lens is None else _ints(lens, "lens", (n,), p.device)
     b.starts = 0 if starts is None else _ints(starts, "starts", (n + 1,), p.device)
@@ -218,7 +219,7 @@ def tq_pages_reserve(p: Pages, table, lens, max_new: int, missing=None):
     if st is not None:
         return _check(st, "tq_pages_reserve")
     _pool(p)
-    b = _batch(p, (1 << 31) - 1, table, lens, None, max_new)
+    b = _batch(p, None, table, lens, None, max_new)
     p.reserve_pool()
     _call(p, "tq_pages_reserve", C.byref(b), _one(missing, "missing", p))
 
@@ -231,7 +232,7 @@ def tq_pages_fork(p: Pages, table, lens, parents, children, missing=None):
     _pool(p)
     n = int(parents.shape[0]) if isinstance(parents, torch.Tensor) and parents.dim() == 1 else -1
     pp, pc = _ints(parents, "parents", (n,), p.device), _ints(children, "children", (n,), p.device)
-    b = _batch(p, 0, table, lens, None, 0)
+    b = _batch(p, None, table, lens, None, 0)
     p.reserve_pool(n)
     _call(p, "tq_pages_fork", C.byref(b), C.c_void_p(pp), C.c_void_p(pc), n, _one(missing, "missing", p))
 
@@ -244,7 +245,7 @@ def tq_pages_free(p: Pages, table, lens, rows):
     _pool(p)
     n = int(rows.shape[0]) if isinstance(rows, torch.Tensor) and rows.dim() == 1 else -1
     pr = _ints(rows, "rows", (n,), p.device)
-    b = _batch(p, 0, table, lens, None, 0)
+    b = _batch(p, None, table, lens, None, 0)
     _call(p, "tq_pages_free", C.byref(b), C.c_void_p(pr), n)
 
 
@@ -254,7 +255,7 @@ def tq_pages_compact(p: Pages, table, n_live=None):
     if st is not None:
         return _check(st, "tq_pages_compact")
     _pool(p)
-    b = _batch(p, 0, table, None, None, 0)
+    b = _batch(p, None, table, None, None, 0)
     p.reserve_pool()
     _call(p, "tq_pages_compact", C.byref(b), _one(n_live, "n_live", p))
 

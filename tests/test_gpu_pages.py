@@ -466,6 +466,24 @@ def test_forks_that_are_skipped():
     assert pool.lens.tolist() == [40, 33, 80, 1, 40, 80, 0, 0, 0]
 
 
+def test_more_new_tokens_than_there_can_be():
+    """max_new is a bound: one of 2^31 - 1 takes no longer."""
+    most = 2**31 - 1
+    rng = np.random.default_rng(35)
+    p, pool = pool_state(rng, 40, 3, 6, 16, heads=1, live=0)
+    pool.lens[:] = [90, 0, 33]
+    table, lens, missing = ints(pool.table), ints(pool.lens), ints([-1])
+    assert pool.reserve(most) == 0
+    tq.tq_pages_reserve(p, table, lens, most, missing=missing)
+    assert same_pool(p, pool, table, lens) and int(missing) == 0
+    x = torch.from_numpy(rng.standard_normal((123, 1, 64)).astype(np.float32)).to(DEV)
+    want = cache64(p)
+    po.append(want, "int8", 16, *[x.double().cpu().numpy()] * 2, pool.table.tolist(), [90, 0, 33], [0, 90, 90, 123])
+    tq.tq_pages_append(p, x, x, table, lens, ints([0, 90, 90, 123]), most)
+    got = cache64(p)
+    assert all(np.array_equal(got[n], want[n]) for n in want)
+
+
 def test_many_forks_in_a_pool_that_runs_out():
     rng = np.random.default_rng(34)
     p, pool = pool_state(rng, 2100, 3003, 4, 16, heads=1, live=3)
