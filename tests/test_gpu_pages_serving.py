@@ -304,3 +304,56 @@ def test_without_the_compiled_half(monkeypatch):
     test_a_serving_run("e4m3")
     test_views_of_wider_arrays()
     T.run_attend(1, 128, 64, "e4m3", "bf16", 2, 4, [1, 33, 64], [1, 1, 1])
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_tables_lengths_and_starts_of_any_value(seed):
+    """No index leaves its array, whatever the device arrays hold: what lies beside every array stays as it was."""
+    rng = np.random.default_rng([67, seed])
+    heads, d, page, n_pages, seqs, width, rows = 2, 64, 16, 12, 5, 6, 40
+
+    def wild(shape, near):
+        x = rng.integers(-2, near + 2, shape)
+        return np.where(rng.random(shape) < 0.3, rng.integers(-2**31, 2**31 - 1, shape), x)
+
+    def guarded(shape, dtype, fill):
+        """A tensor between two stretches of other memory; -> (tensor, check)."""
+        n = int(np.prod(shape))
+        raw = torch.full((n + 2048,), fill, dtype=dtype, device=DEV)
+        return raw[1024:1024 + n].view(shape), lambda: bool((raw[:1024] == fill).all() and (raw[1024 + n:] == fill).all())
+
+    checks = []
+
+    def make(shape, dtype, fill=7):
+        t, ok = guarded(shape, dtype, fill)
+        checks.append(ok)
+        return t
+
+    def put(values, dtype=torch.int32):
+        t = make(np.shape(values), dtype)
+        t.copy_(torch.from_numpy(np.asarray(values)).to(dtype))
+        return t
+
+    k, v = (make((n_pages, heads, page, d), torch.int8) for _ in range(2))
+    scales = [make((n_pages, heads), torch.float32, 1.0) for _ in range(2)]
+    p = tq.Pages(k, v, *scales, bounds=make((n_pages, heads, 2, d), torch.bfloat16, 1.0), refs=put(rng.integers(0, 2, n_pages)))
+    for dtype in (torch.float32, torch.bfloat16):
+        for most in (1, 9, 100):
+            table, lens = put(wild((seqs, width), n_pages)), put(wild(seqs, width * page))
+            starts = put(np.sort(wild(seqs + 1, rows)) if seed % 2 else wild(seqs + 1, rows))
+            x = torch.randn((rows, heads, d), device=DEV).to(dtype)
+            q = torch.randn((rows, heads * 2, d), device=DEV).to(dtype)
+            out, lse = make((rows, heads * 2, d), dtype, 5.0), make((rows, heads * 2), torch.float32, 5.0)
+            chosen = put(wild((rows, heads, 7), width))
+            tq.tq_pages_append(p, x, x, table, lens, starts, most)
+            for window in (0, 3):
+                tq.tq_pages_attend(p, q, table, lens, starts, most, 0.1, out, lse=lse, window=window)
+                tq.tq_pages_attend(p, q, table, lens, starts, most, 0.1, out, lse=lse, window=window, chosen=chosen)
+            tq.tq_pages_select(p, q, table, lens, starts, most, chosen)
+            tq.tq_pages_reserve(p, table, lens, most)
+            tq.tq_pages_fork(p, table, lens, put(wild(6, seqs)), put(wild(6, seqs)))
+            tq.tq_pages_free(p, table, lens, put(wild(4, seqs)))
+            tq.tq_pages_compact(p, table)
+            tq.tq_pages_copy(p, put(wild(1, n_pages)), put(wild(1, n_pages)))
+            torch.cuda.synchronize()
+            assert all(ok() for ok in checks)
