@@ -56,7 +56,7 @@ template <int D, bool F32, int G>
 __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs a, const int blocks, const int steps) {
   constexpr int C = D / 16;                 // channels of a lane
   constexpr int U = pages_at_once(G), V = U * G;
-  __shared__ double q_s[G][C][16];
+  __shared__ double q_s[G][C][16][2];  // what is positive of a query's value, and what is negative: q_j > 0 ? q_j upper_j : q_j lower_j is a sum of two
   const int heads = a.c.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & 15, lanes = lane >> 4;
   const int block = (int)(blockIdx.x % (unsigned)blocks);
   unsigned unit = blockIdx.x / (unsigned)blocks;
@@ -78,7 +78,9 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
   const auto stage = [&](int g0) {
     for (int i = threadIdx.x; i < G * D; i += 256) {
       const int g = g0 + i / D < a.group ? g0 + i / D : a.group - 1, c = i % D;
-      q_s[i / D][c % C][c / C] = (double)load_value(a.q.p, row * a.q.ld_row + (h * a.group + g) * a.q.ld_head + c, F32);
+      const double x = (double)load_value(a.q.p, row * a.q.ld_row + (h * a.group + g) * a.q.ld_head + c, F32);
+      q_s[i / D][c % C][c / C][0] = x > 0. ? x : 0.;
+      q_s[i / D][c % C][c / C][1] = x > 0. ? 0. : x;  // (NaN is kept)
     }
     __syncthreads();
   };
@@ -111,21 +113,25 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
         __syncthreads();
         stage(g0);
       }
+      // (else the compiler turns all channels before the loop over the heads, into 64 to 256 registers)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int c = 0; c < C / 2; ++c) asm("" : "+v"(lo[u][c]), "+v"(hi[u][c]));
       double sum[V] = {};
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float low[U], high[U];
+        double low[U], high[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          low[u] = __uint_as_float((c & 1) ? lo[u][c / 2] & 0xffff0000u : lo[u][c / 2] << 16);
-          high[u] = __uint_as_float((c & 1) ? hi[u][c / 2] & 0xffff0000u : hi[u][c / 2] << 16);
+          low[u] = (double)__uint_as_float((c & 1) ? lo[u][c / 2] & 0xffff0000u : lo[u][c / 2] << 16);
+          high[u] = (double)__uint_as_float((c & 1) ? hi[u][c / 2] & 0xffff0000u : hi[u][c / 2] << 16);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const double f = q_s[g][c][j];
-          const bool positive = f > 0.;
+          const double above = q_s[g][c][j][0], below = q_s[g][c][j][1];
 #pragma unroll
-          for (int u = 0; u < U; ++u) sum[u * G + g] = fma(f, (double)(positive ? high[u] : low[u]), sum[u * G + g]);
+          for (int u = 0; u < U; ++u) sum[u * G + g] = fma(above, high[u], fma(below, low[u], sum[u * G + g]));
         }
       }
       add_halves<8, ROR8, V>(sum);
@@ -156,6 +162,17 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
   }
 }
 
+// sums of the lanes up to and with this one
+__device__ __forceinline__ int scan_wavefront(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next, of two rows to the next two
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 template <int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectArgs a) {
   constexpr int WAVES = THREADS / 64;
@@ -169,18 +186,20 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
   const int h = (int)(unit % (unsigned)heads);
   unit /= (unsigned)heads;
   const int s = (int)(unit / (unsigned)a.b.max_new), t = (int)(unit % (unsigned)a.b.max_new);
-  const int whole = a.b.count(s), len = a.b.lens[s];
+  const int whole = a.b.count(s);
   const int64_t row = a.b.first_row(s) + t;
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
-  const int pos = len - whole + t;
-  const int n = pos >= 0 ? min((pos >> a.c.log2_page) + 1, a.b.width) : 0;
   const uint32_t* const words = reinterpret_cast<const uint32_t*>(a.scores) + (row * heads + h) * a.b.width;
   int32_t* const out = a.chosen + (row * heads + h) * a.n_chosen;
 
   // places tid, tid + THREADS, ..: the first HELD of a thread in registers
   uint32_t held[HELD];
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < n ? words[i * THREADS + tid] : 0u;
+  for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < a.b.width ? words[i * THREADS + tid] : 0u;
+  const int pos = a.b.lens[s] - whole + t;
+  const int n = pos >= 0 ? min((pos >> a.c.log2_page) + 1, a.b.width) : 0;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < n ? held[i] : 0u;  // (behind the row's last page nothing has been written)
   const auto each = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < HELD; ++i) f(held[i]);
@@ -225,12 +244,7 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
       int c[4], sum = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[i] = count_s[pass][255 - 4 * lane - i], sum += c[i];
-      int upto = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(upto, o);
-        if (lane >= o) upto += v;
-      }
+      const int upto = scan_wavefront(sum);
       int over = upto - sum, value = 0, here = 0, many = 0;
       bool mine = false;
 #pragma unroll
@@ -266,12 +280,7 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
     }
     __syncthreads();
     const int own = lane < HELD * WAVES ? sum_s[lane] : 0;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < HELD * WAVES; o <<= 1) {
-      const int v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
-    }
+    int upto = scan_wavefront(own);
     const int all = __builtin_amdgcn_readlane(upto, HELD * WAVES - 1);
     upto -= own;
 #pragma unroll
