@@ -395,45 +395,74 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAtt
   }
 }
 
-// one wavefront for each row and head: the ranges of keys in one frame
-template <int D, bool F32>
+// The ranges of keys of a row and head in one frame: one wavefront for up to 16 of them, four (WIDE) for up to 64, 16 to each
+// (32 ranges of 32 rows 4.0 -> 3.6 us, traced).
+template <int D, bool F32, bool WIDE>
 __global__ __launch_bounds__(256) void pages_join_kernel(const PagesAttendArgs a) {
   constexpr int VE = D / 64;
-  const int lane = threadIdx.x & 63, heads = a.c.heads * a.group;
-  int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ float y_s[WIDE ? 4 : 1][WIDE ? D + 4 : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.c.heads * a.group;
+  int64_t item = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   const int head = (int)(item % heads);
   item /= heads;
   const int s = (int)(item / a.b.max_new), t = (int)(item % a.b.max_new);
   if (s >= a.b.n_seqs || t >= a.b.count(s)) return;
   const int64_t row = a.b.first_row(s) + t;
   if (row < 0 || row >= a.b.n_rows) return;
-  const float* const part = a.part + (row * heads + head) * a.splits * kPart<D>;
-  // 16 ranges on their way at a time, the first before anything is waited for
+  const int i0 = WIDE ? 16 * wave : 0, n = min(a.splits - i0, 16);  // this wavefront's ranges
+  const float* const part = a.part + ((row * heads + head) * a.splits + i0) * kPart<D>;
+  // everything is asked for before anything is waited for
   float x[16][VE];
-  const auto fetch = [&](int i0) {
+  float m = -INFINITY, l = 0.f;
+  if (n > 0) {
+    if (lane < n) m = part[lane * kPart<D>], l = part[lane * kPart<D> + 1];
 #pragma unroll
     for (int u = 0; u < 16; ++u)
 #pragma unroll
-      for (int c = 0; c < VE; ++c) x[u][c] = part[(i0 + u < a.splits ? i0 + u : 0) * kPart<D> + 4 + lane * VE + c];
-  };
-  float m = -INFINITY, l = 0.f;
-  if (lane < a.splits) m = part[lane * kPart<D>], l = part[lane * kPart<D> + 1];
-  fetch(0);
-  const float top = over_wavefront(m, [](float p, float q) { return fmaxf(p, q); });
+      for (int c = 0; c < VE; ++c) x[u][c] = part[(u < n ? u : 0) * kPart<D> + 4 + lane * VE + c];
+  }
+  float top = over_wavefront(m, [](float p, float q) { return fmaxf(p, q); });
   const float f = l == 0.f ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-  const float sum = over_wavefront(f * l, [](float p, float q) { return p + q; });
+  float sum = over_wavefront(f * l, [](float p, float q) { return p + q; });
   float y[VE] = {};
-  for (int i0 = 0; i0 < a.splits; i0 += 16) {
+  if (n > 0) {
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
-      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i0 + u));  // (0 behind the last range)
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), u));  // (0 behind the last range)
 #pragma unroll
       for (int c = 0; c < VE; ++c) y[c] = fmaf(w, x[u][c], y[c]);
     }
-    if (i0 + 16 < a.splits) fetch(i0 + 16);
+  }
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int c = 0; c < VE; ++c) y_s[wave][4 + lane * VE + c] = y[c];
+    if (lane == 0) y_s[wave][0] = top, y_s[wave][1] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+    float mw[4], lw[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mw[w] = y_s[w][0], lw[w] = y_s[w][1];
+    top = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3]));
+    sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < VE; ++c) y[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float fw = lw[w] == 0.f ? 0.f : mw[w] == top ? 1.f : __builtin_amdgcn_exp2f(mw[w] - top);
+      sum = fmaf(fw, lw[w], sum);
+#pragma unroll
+      for (int c = 0; c < VE; ++c) y[c] = fmaf(fw, y_s[w][4 + lane * VE + c], y[c]);
+    }
   }
   store_row<VE, F32>(a.out, row, head, lane * VE, y, sum);
   if (a.lse != nullptr && lane == 0) a.lse[row * heads + head] = log_sum(top, sum);
+}
+
+template <int D, bool F32>
+void launch_join(const PagesAttendArgs& a, hipStream_t s) {
+  const int64_t items = (int64_t)a.b.n_seqs * a.b.max_new * a.c.heads * a.group;
+  if (a.splits > 16) hipLaunchKernelGGL((pages_join_kernel<D, F32, true>), dim3((unsigned)items), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((pages_join_kernel<D, F32, false>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
 }
 
 template <int D, int CT>
@@ -452,9 +481,8 @@ hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.splits == 1) return e;
-  const dim3 join((unsigned)(((int64_t)a.b.n_seqs * a.b.max_new * a.c.heads * a.group + 3) / 4));
-  if (f32) hipLaunchKernelGGL((pages_join_kernel<D, true>), join, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((pages_join_kernel<D, false>), join, dim3(256), 0, s, a);
+  if (f32) launch_join<D, true>(a, s);
+  else launch_join<D, false>(a, s);
   return hipGetLastError();
 }
 
