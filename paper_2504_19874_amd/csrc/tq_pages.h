@@ -34,6 +34,19 @@ struct BatchView {
   __device__ __forceinline__ int count(int s) const { return starts != nullptr ? starts[s + 1] - starts[s] : max_new; }
 };
 
+// Numbers below 2^31 over one that the host knows: a product's upper half, a sum and a shift (scalar where the number is; the compiler's own
+// division of two registers is some thirty vector instructions, of 64 bits over a hundred, in front of a kernel's first load).
+struct Divide {
+  uint32_t mul, shift, by;
+  Divide() = default;
+  explicit Divide(int64_t d) : mul(0), shift(0), by((uint32_t)(d > 0 ? d : 1)) {
+    while ((1ull << shift) < by) ++shift;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+  __device__ __forceinline__ uint32_t rest(uint32_t n, uint32_t quotient) const { return n - quotient * by; }
+};
+
 // Rows of keys, values, queries or outputs.
 struct PagesRows {
   const void* p;
@@ -86,6 +99,7 @@ struct PagesAttendArgs {
   bool prompt;  // the kernel for prompts
   int tiles;    // of 16 rows to a workgroup of the other kernel
   float* part;  // what they leave, [n_rows][query heads][splits][4 + d]; with one range unused
+  Divide by_splits, by_tiles, by_heads, by_new, by_group, by_queries;  // (tiles of rows: of the kernel that is taken; query heads)
 };
 // workgroups of one range each: sequences (or rows) times heads times tiles of query rows
 int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen, int tiles);
@@ -98,6 +112,7 @@ size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, 
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
 // many rows of bf16 queries (tq_pages_attend_prompt.hip)
 hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s);
+constexpr int pages_prompt_rows(int d) { return d == 256 ? 128 : 256; }  // to a workgroup
 
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,
                                hipStream_t s);
@@ -109,6 +124,7 @@ struct PagesSelectArgs {
   int group, keep_first, keep_last, n_chosen;
   int32_t* chosen;
   float* scores;  // [n_rows][heads][width]
+  Divide by_heads, by_new, by_blocks;  // (blocks: workgroups that score the pages of a row and head)
 };
 hipError_t launch_pages_select(int d, bool f32, const PagesSelectArgs& a, hipStream_t s);
 

@@ -208,6 +208,7 @@ tq_status tq_pages_reserve(const tq_pages* c, const tq_batch* b, int32_t* missin
   tq_status st = check_pool(c, b, 0);
   if (st != TQ_OK) return st;
   if (b->n_seqs > 0 && !batch_arrays(b)) return TQ_ERR_INVALID_ARG;
+  if (!launchable((int64_t)b->n_seqs + 1024, std::min<int64_t>(b->max_new / c->page_tokens + 2, std::max(b->width, 1)), 1)) return TQ_ERR_UNSUPPORTED;
   return from_hip(launch_pages_reserve(view(c), view(b), static_cast<int32_t*>(c->workspace), missing, static_cast<hipStream_t>(stream)));
 }
 

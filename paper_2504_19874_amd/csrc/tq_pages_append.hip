@@ -71,18 +71,19 @@ __device__ __forceinline__ float outward(float x, bool down) {
 
 template <int D, int CT, bool F32, int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_append_kernel(const PagesView c, const BatchView b, const PagesRows kr, const PagesRows vr,
-                                                              const int pages_each) {
+                                                              const Divide pages_each) {
   constexpr int COLS = D / 8, LINES = THREADS / COLS;  // threads of a row, rows at a time
   __shared__ uint32_t red_s[THREADS / 64];
   __shared__ float edge_s[2][LINES][D];
   const int tid = threadIdx.x, col = tid % COLS, line = tid / COLS;
-  const int s = (int)(blockIdx.x / (unsigned)pages_each), h = blockIdx.y;
+  const uint32_t seq = pages_each.of(blockIdx.x);
+  const int s = (int)seq, h = blockIdx.y;
   const bool values = blockIdx.z != 0;
   const int page = 1 << c.log2_page;
   const int len = b.lens[s], count = b.count(s);
   const int64_t begin = (int64_t)len - count;  // position of the sequence's first row
   const int64_t first = begin > 0 ? begin : 0;
-  const int64_t index = (first >> c.log2_page) + blockIdx.x % (unsigned)pages_each, at = index << c.log2_page;
+  const int64_t index = (first >> c.log2_page) + pages_each.rest(blockIdx.x, seq), at = index << c.log2_page;
   // positions [lo, hi) of this page are new (no more than max_new rows of a sequence are taken)
   const int64_t end = count > b.max_new ? begin + b.max_new : (int64_t)len;
   const int64_t row0 = b.first_row(s);
@@ -231,7 +232,7 @@ hipError_t launch(const PagesView& c, const BatchView& b, const PagesRows& k, co
   int64_t pages_each = (((int64_t)b.max_new + (1 << c.log2_page) - 2) >> c.log2_page) + 1;
   if (pages_each > b.width) pages_each = b.width;
   const dim3 grid((unsigned)(b.n_seqs * pages_each), (unsigned)c.heads, 2);
-  hipLaunchKernelGGL((pages_append_kernel<D, CT, F32, 256>), grid, dim3(256), 0, s, c, b, k, v, (int)pages_each);
+  hipLaunchKernelGGL((pages_append_kernel<D, CT, F32, 256>), grid, dim3(256), 0, s, c, b, k, v, Divide(pages_each));
   return hipGetLastError();
 }
 

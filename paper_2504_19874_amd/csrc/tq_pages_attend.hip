@@ -64,30 +64,31 @@ struct Walk {
 
   __device__ __forceinline__ explicit Walk(const PagesAttendArgs& args) : a(args) {}
 
-  __device__ __forceinline__ int64_t row_of(int m) const { return row0 + t0 + m / a.group; }
-  __device__ __forceinline__ int head_of(int m) const { return h * a.group + m % a.group; }
+  __device__ __forceinline__ int token_of(int m) const { return (int)a.by_group.of((uint32_t)m); }
+  __device__ __forceinline__ int64_t row_of(int m) const { return row0 + t0 + token_of(m); }
+  __device__ __forceinline__ int head_of(int m) const { return h * a.group + m - token_of(m) * a.group; }
 
   // the unit and its rows [first, first + 16 R); false: there are none
   __device__ __forceinline__ bool start(unsigned unit, int first_row) {
     lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     heads = a.c.heads;
-    h = (int)(unit % (unsigned)heads);
-    unit /= (unsigned)heads;
-    const int s = a.chosen != nullptr ? (int)(unit / (unsigned)a.b.max_new) : (int)unit;
-    t0 = a.chosen != nullptr ? (int)(unit % (unsigned)a.b.max_new) : 0;
+    const uint32_t rest = a.by_heads.of(unit);
+    h = (int)a.by_heads.rest(unit, rest);
+    const int s = a.chosen != nullptr ? (int)a.by_new.of(rest) : (int)rest;
+    t0 = a.chosen != nullptr ? (int)a.by_new.rest(rest, (uint32_t)s) : 0;
     const int whole = a.b.count(s), count = min(whole, a.b.max_new);
     rows = (a.chosen != nullptr ? (t0 < count ? 1 : 0) : count) * a.group;
     if (first_row >= rows) return false;
     const int len = a.b.lens[s];
     row0 = a.b.first_row(s);
     const int at0 = len - whole + t0;
-    pos_lo = at0 + first_row / a.group, pos_hi = at0 + min(first_row + 16 * R - 1, rows - 1) / a.group;
+    pos_lo = at0 + token_of(first_row), pos_hi = at0 + token_of(min(first_row + 16 * R - 1, rows - 1));
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int m = min(first_row + 16 * i + r, rows - 1);
       const int64_t row = row_of(m);
       const bool there = first_row + 16 * i + r < rows && row >= 0 && row < a.b.n_rows;
-      pos[i] = at0 + m / a.group;
+      pos[i] = at0 + token_of(m);
       load_query(i, there, row * a.q.ld_row + head_of(m) * a.q.ld_head + g * (D / 4));
 #pragma unroll
       for (int e = 0; e < VE; ++e) o[i][e] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -323,12 +324,10 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_kernel(const PagesAtt
   __shared__ float o_s[2][16][D + 4];
   __shared__ float ml_s[WAVES][16][2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row_tiles = (int)(((a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group + 16 * R - 1) / (16 * R));
-  const int split = (int)(blockIdx.x % (unsigned)a.splits);
-  const unsigned unit = blockIdx.x / (unsigned)a.splits;
-  const int tile = (int)(unit % (unsigned)row_tiles);
+  const uint32_t ranged = a.by_splits.of(blockIdx.x), unit = a.by_tiles.of(ranged);
+  const int split = (int)a.by_splits.rest(blockIdx.x, ranged), tile = (int)a.by_tiles.rest(ranged, unit);
   Walk<D, CT, F32, R> w(a);
-  if (!w.start(unit / (unsigned)row_tiles, 16 * R * tile)) return;
+  if (!w.start(unit, 16 * R * tile)) return;
   // this wavefront's tiles: an equal part of them, in one piece
   const int tiles = w.tiles(), each = (tiles + a.splits * WAVES - 1) / (a.splits * WAVES);
   const int begin = (split * WAVES + wave) * each;
@@ -402,10 +401,8 @@ __global__ __launch_bounds__(256) void pages_join_kernel(const PagesAttendArgs a
   constexpr int VE = D / 64;
   __shared__ float y_s[WIDE ? 4 : 1][WIDE ? D + 4 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.c.heads * a.group;
-  int64_t item = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  const int head = (int)(item % heads);
-  item /= heads;
-  const int s = (int)(item / a.b.max_new), t = (int)(item % a.b.max_new);
+  const uint32_t item = WIDE ? blockIdx.x : blockIdx.x * 4 + (uint32_t)wave, token = a.by_queries.of(item);
+  const int head = (int)a.by_queries.rest(item, token), s = (int)a.by_new.of(token), t = (int)a.by_new.rest(token, (uint32_t)s);
   if (s >= a.b.n_seqs || t >= a.b.count(s)) return;
   const int64_t row = a.b.first_row(s) + t;
   if (row < 0 || row >= a.b.n_rows) return;
@@ -466,7 +463,10 @@ void launch_join(const PagesAttendArgs& a, hipStream_t s) {
 }
 
 template <int D, int CT>
-hipError_t launch(bool f32, const PagesAttendArgs& a, hipStream_t s) {
+hipError_t launch(bool f32, PagesAttendArgs a, hipStream_t s) {
+  const int64_t rows = (a.chosen != nullptr ? 1 : (int64_t)a.b.max_new) * a.group, per = a.prompt ? pages_prompt_rows(D) : 16 * a.tiles;
+  a.by_splits = Divide(a.splits), a.by_tiles = Divide((rows + per - 1) / per);
+  a.by_heads = Divide(a.c.heads), a.by_new = Divide(a.b.max_new), a.by_group = Divide(a.group), a.by_queries = Divide(a.c.heads * a.group);
   hipError_t e;
   if (a.prompt) {
     e = launch_pages_attend_prompt(D, CT, a, s);
@@ -509,7 +509,7 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 920 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
   // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577;
   // d = 256, where a workgroup has 128 rows: 427 of 1191 129 / 153, 500 of 1000 72 / 64
-  const int64_t block = d == 256 ? 128 : 256, blocks = (int64_t)b.n_seqs * heads * ((rows + block - 1) / block);
+  const int64_t block = pages_prompt_rows(d), blocks = (int64_t)b.n_seqs * heads * ((rows + block - 1) / block);
   if (!chosen && !f32 && rows > 64) {
     const int64_t fill = (device_cu_count() + blocks - 1) / blocks, most = (keys + 1023) / 1024;
     plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)16);

@@ -24,12 +24,13 @@ constexpr int WAVES = 8;
 template <int D>
 constexpr int kShare = D == 256 ? 2 : 1;
 template <int D>
-constexpr int kRows = 32 * WAVES / kShare<D>;
+constexpr int kRows = pages_prompt_rows(D);
 
 template <int D, int CT>
 __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const PagesAttendArgs a) {
   constexpr int KS = D / 16;             // k steps of S
   constexpr int ROWS = kRows<D>;
+  static_assert(ROWS == 32 * WAVES / kShare<D>, "32 rows to a wavefront, or to two");
   constexpr int DA = D / 32, DT = DA / kShare<D>;  // d tiles, and those of a wavefront
   constexpr int KC = D == 64 ? 4 : D == 128 ? 8 : 4;  // fragments of keys that a lane holds at a time (d = 256: 8 cost 8 % by spills)
   constexpr int VW = D == 256 ? 2 : 1;   // words of a key's values that a lane turns
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   __shared__ uint16_t poison_s[2][4];    // of a subtile's keys: those with a NaN among their values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, b = lane >> 5;
   const int heads = a.c.heads, group = a.group;
-  const int row_tiles = (int)(((int64_t)a.b.max_new * group + ROWS - 1) / ROWS);
+  const int row_tiles = (int)a.by_tiles.by;
   // the row tiles of a unit read the same keys: on one XCD (workgroups go to the eight of them in turn), the longest first
   const unsigned units = (unsigned)a.b.n_seqs * (unsigned)heads, each_unit = (unsigned)(row_tiles * a.splits);
   unsigned unit, part_of;
@@ -51,16 +52,17 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   if (first >= rows) return;
   const int len = a.b.lens[s];
   const int64_t row0 = a.b.first_row(s);
+  const auto token_of = [&](int m) { return (int)a.by_group.of((uint32_t)m); };
   const int at0 = len - whole;
 
   const int rows_of = kShare<D> == 1 ? wave : wave & 3, dh = kShare<D> == 1 ? 0 : wave >> 2;  // which 32 rows, which part of the coordinates
   const int m = min(first + 32 * rows_of + r, rows - 1);
-  const int64_t row = row0 + m / group;
-  const int head = h * group + m % group;
+  const int64_t row = row0 + token_of(m);
+  const int head = h * group + m - token_of(m) * group;
   const bool there = first + 32 * rows_of + r < rows && row >= 0 && row < a.b.n_rows;
-  const int pos = at0 + m / group;
-  const int pos_lo = at0 + first / group, pos_hi = at0 + min(first + ROWS - 1, rows - 1) / group;  // of the workgroup
-  const int mine_lo = at0 + min(first + 32 * rows_of, rows - 1) / group, mine_hi = at0 + min(first + 32 * rows_of + 31, rows - 1) / group;
+  const int pos = at0 + token_of(m);
+  const int pos_lo = at0 + token_of(first), pos_hi = at0 + token_of(min(first + ROWS - 1, rows - 1));  // of the workgroup
+  const int mine_lo = at0 + token_of(min(first + 32 * rows_of, rows - 1)), mine_hi = at0 + token_of(min(first + 32 * rows_of + 31, rows - 1));
 
   bf16x8_t q[KS];
 #pragma unroll

@@ -42,24 +42,24 @@ __device__ __forceinline__ int free_pages(const PagesView& c, int want, int32_t*
 
 __device__ __forceinline__ bool is_page(const PagesView& c, int p) { return p >= 0 && p < c.n_pages; }
 
-__global__ __launch_bounds__(THREADS) void pages_reserve_kernel(const PagesView c, const BatchView b, const int each, int32_t* list,
+__global__ __launch_bounds__(THREADS) void pages_reserve_kernel(const PagesView c, const BatchView b, const Divide each, int32_t* list,
                                                                int32_t* missing) {
   __shared__ int wave_s[WAVES];
-  const int64_t items = (int64_t)b.n_seqs * each;
-  const auto entry = [&](int64_t item) -> int32_t* {
+  const uint32_t items = (uint32_t)b.n_seqs * each.by;
+  const auto entry = [&](uint32_t item) -> int32_t* {
     if (item >= items) return nullptr;
-    const int s = (int)(item / each);
+    const uint32_t s = each.of(item);
     const int64_t len = b.lens[s], from = len > b.max_new ? len - b.max_new : 0;
-    const int64_t i = (from >> c.log2_page) + item % each;
+    const int64_t i = (from >> c.log2_page) + each.rest(item, s);
     if ((i << c.log2_page) >= len || i >= b.width) return nullptr;
     int32_t* const e = b.table + (int64_t)s * b.table_stride + i;
     return is_page(c, *e) ? nullptr : e;
   };
   int want = 0;
-  for (int64_t i = 0; i < items; i += THREADS) rank_of(entry(i + threadIdx.x) != nullptr, want, wave_s);
+  for (uint32_t i = 0; i < items; i += THREADS) rank_of(entry(i + threadIdx.x) != nullptr, want, wave_s);
   const int got = free_pages(c, want, list, wave_s);
   int at = 0;
-  for (int64_t i = 0; i < items; i += THREADS) {
+  for (uint32_t i = 0; i < items; i += THREADS) {
     int32_t* const e = entry(i + threadIdx.x);
     const int rank = rank_of(e != nullptr, at, wave_s);
     if (e != nullptr) {
@@ -254,7 +254,7 @@ hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t*
   // max_new positions lie in no more pages than this, nor in more than a sequence has entries
   int64_t each = (((int64_t)b.max_new + (1 << c.log2_page) - 2) >> c.log2_page) + 1;
   each = each < b.width ? each : b.width > 0 ? b.width : 1;
-  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(THREADS), 0, s, c, b, (int)each, list, missing);
+  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(THREADS), 0, s, c, b, Divide(each), list, missing);
   return hipGetLastError();
 }
 

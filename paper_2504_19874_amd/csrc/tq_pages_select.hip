@@ -53,16 +53,14 @@ __device__ __forceinline__ void add_halves(double (&v)[V]) {
 constexpr int pages_at_once(int heads) { return heads == 1 ? 8 : 4; }  // of a group of 16 lanes: 8 sums, or 16 for four heads
 
 template <int D, bool F32, int G>
-__global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs a, const int blocks, const int steps) {
+__global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs a, const int steps) {
   constexpr int C = D / 16;                 // channels of a lane
   constexpr int U = pages_at_once(G), V = U * G;
   __shared__ double q_s[G][C][16][2];  // what is positive of a query's value, and what is negative: q_j > 0 ? q_j upper_j : q_j lower_j is a sum of two
   const int heads = a.c.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & 15, lanes = lane >> 4;
-  const int block = (int)(blockIdx.x % (unsigned)blocks);
-  unsigned unit = blockIdx.x / (unsigned)blocks;
-  const int h = (int)(unit % (unsigned)heads);
-  unit /= (unsigned)heads;
-  const int s = (int)(unit / (unsigned)a.b.max_new), t = (int)(unit % (unsigned)a.b.max_new);
+  const uint32_t unit = a.by_blocks.of(blockIdx.x), new_row = a.by_heads.of(unit);
+  const int block = (int)a.by_blocks.rest(blockIdx.x, unit), h = (int)a.by_heads.rest(unit, new_row);
+  const int s = (int)a.by_new.of(new_row), t = (int)a.by_new.rest(new_row, (uint32_t)s);
   const int whole = a.b.count(s);
   const int64_t row = a.b.first_row(s) + t;
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
@@ -182,10 +180,8 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
   __shared__ int kept_s[2][WAVES];
   __shared__ uint32_t range_s[2][WAVES];
   const int heads = a.c.heads, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  unsigned unit = blockIdx.x;
-  const int h = (int)(unit % (unsigned)heads);
-  unit /= (unsigned)heads;
-  const int s = (int)(unit / (unsigned)a.b.max_new), t = (int)(unit % (unsigned)a.b.max_new);
+  const uint32_t new_row = a.by_heads.of(blockIdx.x);
+  const int h = (int)a.by_heads.rest(blockIdx.x, new_row), s = (int)a.by_new.of(new_row), t = (int)a.by_new.rest(new_row, (uint32_t)s);
   const int whole = a.b.count(s);
   const int64_t row = a.b.first_row(s) + t;
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
@@ -295,7 +291,7 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
 }
 
 template <int D, bool F32, int G>
-hipError_t launch_score(const PagesSelectArgs& a, int64_t units, hipStream_t s) {
+hipError_t launch_score(PagesSelectArgs a, int64_t units, hipStream_t s) {
   // a wavefront takes a step (16 or 32 pages), up to eight where that leaves three workgroups for a compute unit.  Four rows of 8 heads and
   // 2048 pages, both kernels: one 25.2 us, two 21.2, three and more 19.3
   constexpr int per = 4 * 4 * pages_at_once(G);
@@ -303,7 +299,8 @@ hipError_t launch_score(const PagesSelectArgs& a, int64_t units, hipStream_t s) 
   int64_t steps = units * all / (3 * device_cu_count());
   steps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
   const int64_t blocks = (all + steps - 1) / steps;
-  hipLaunchKernelGGL((pages_score_kernel<D, F32, G>), dim3((unsigned)(units * blocks)), dim3(256), 0, s, a, (int)blocks, (int)steps);
+  a.by_blocks = Divide(blocks);
+  hipLaunchKernelGGL((pages_score_kernel<D, F32, G>), dim3((unsigned)(units * blocks)), dim3(256), 0, s, a, (int)steps);
   return hipGetLastError();
 }
 template <int D, bool F32>
@@ -314,7 +311,8 @@ hipError_t launch_score_g(const PagesSelectArgs& a, int64_t units, hipStream_t s
 }
 
 template <int D>
-hipError_t launch(bool f32, const PagesSelectArgs& a, hipStream_t s) {
+hipError_t launch(bool f32, PagesSelectArgs a, hipStream_t s) {
+  a.by_heads = Divide(a.c.heads), a.by_new = Divide(a.b.max_new);
   const int64_t units = (int64_t)a.b.n_seqs * a.b.max_new * a.c.heads;
   if (a.b.width > 0) {
     const hipError_t e = f32 ? launch_score_g<D, true>(a, units, s) : launch_score_g<D, false>(a, units, s);
