@@ -1,16 +1,22 @@
 // Attention over pages for prompts: many rows of bf16 queries.
 //
 // The mathematics is that of tq_pages_attend.hip.  Here a workgroup has 256 rows (d = 256: 128) of a sequence and head, 32 to a wavefront, and all
-// wavefronts share one tile of 64 keys in LDS, as 16-bit operands: turning codes into operands (and values by 4 x 4 bytes) is
+// wavefronts share one tile of 128 keys (d = 256: 64) in LDS, as 16-bit operands: turning codes into operands (and values by 4 x 4 bytes) is
 // vector work that eight wavefronts would do eight times.  Products on v_mfma_f32_32x32x16, S^T = K Q^T and O^T += V^T P^T:
 // lane (r = lane % 32, b = lane / 32) has row r and of 16 keys 4 b + 0..3 and 8 + 4 b + 0..3 in both, so weights stay in
 // their lane.  LDS holds fragments in the order in which the lanes read them (16 bytes a lane, 1 KB a product):
 //   keys    [32 keys][16 coordinates][lane]: lane (key, half of the coordinates), its place XOR the coordinates' number, so that eight
 //           lanes that write one key's fragments meet eight groups of banks
-//   values  [16 keys][d tile][lane]: d tile T has the coordinates (d / 32) i + T; a lane fetches d / 32 coordinates of eight keys and
-//           writes a fragment to each d tile (d = 64: four coordinates, two to each)
-// Wavefronts 0..3 take the values of one subtile of 16 keys each, 4..7 the keys.  The next tile is fetched while a tile is multiplied
+//   values  [16 keys][d tile][lane]: d tile t has the coordinates (d / 32) i + t; a lane fetches d / 32 coordinates of eight keys and
+//           writes a fragment to each d tile (d = 64: four coordinates, two to each, and half a wavefront has a subtile of 16 keys)
+// Wavefronts 0..3 take the values of two subtiles of 16 keys each (d = 256: one), 4..7 the keys.  The next tile is fetched while a tile is multiplied
 // and written to the other half of LDS: one barrier a tile.
+//
+// What bounds it: matrix and vector instructions hardly run at the same time with two wavefronts to a SIMD (measured: 16 fused
+// multiply-adds behind every product take 29.7 ns, apart 17.1 and 13.7; only exponentials hide), so what counts is the number of vector
+// instructions.  Tiles of 128 keys have half the barriers, addresses and masks of tiles of 64: 8192 tokens of which 2048 are new, 4
+// sequences of 8 x 4 heads, d = 64 784 -> 620 us, d = 128 1012 -> 970 (on one card); d = 256 1614 -> 1390 (two sequences) by what
+// is no longer carried through the loop in registers.  Logits of the next 32 keys multiplied between the exponentials: 7-15 % slower.
 #include "tq_pages_attend.h"
 
 namespace tq {
@@ -26,6 +32,10 @@ constexpr int kShare = D == 256 ? 2 : 1;
 template <int D>
 constexpr int kRows = pages_prompt_rows(D);
 
+// subtiles of 16 keys of a tile: LDS holds two tiles (d = 64: 16 are not faster)
+template <int D>
+constexpr int kSubtiles = D == 256 ? 4 : 8;
+
 template <int D, int CT>
 __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const PagesAttendArgs a) {
   constexpr int KS = D / 16;             // k steps of S
@@ -34,10 +44,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   constexpr int DA = D / 32, DT = DA / kShare<D>;  // d tiles, and those of a wavefront
   constexpr int KC = D == 64 ? 4 : D == 128 ? 8 : 4;  // fragments of keys that a lane holds at a time (d = 256: 8 cost 8 % by spills)
   constexpr int VW = D == 256 ? 2 : 1;   // words of a key's values that a lane turns
-  constexpr int KL = D / 64;             // 16-byte loads of a lane's keys
-  constexpr int TILE = 64 * D * 2 / 16;  // fragments of a tile's keys, as many of its values
+  constexpr int T = kSubtiles<D>, SW = T / 4;  // subtiles of 16 keys of a tile, and those of a wavefront that turns codes
+  constexpr int VQ = D == 64 ? 1 : SW;   // ... one after the other (d = 64: half a wavefront has one)
+  constexpr int KL = D / 64;             // 16-byte loads of a lane's keys of a subtile
+  constexpr int TILE = 16 * T * D * 2 / 16;  // fragments of a tile's keys, as many of its values
   extern __shared__ uint4_t lds[];       // [2][keys, values][TILE]
-  __shared__ uint16_t poison_s[2][4];    // of a subtile's keys: those with a NaN among their values
+  __shared__ uint16_t poison_s[2][T];    // of a subtile's keys: those with a NaN among their values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, b = lane >> 5;
   const int heads = a.c.heads, group = a.group;
   const int row_tiles = (int)a.by_tiles.by;
@@ -79,31 +91,37 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
   const int hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 128));
   const int lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~63;
-  const int all_tiles = hi > lo ? (hi - lo + 63) >> 6 : 0, each = (all_tiles + a.splits - 1) / a.splits;
+  const int all_tiles = hi > lo ? (int)(((int64_t)hi - lo + 16 * T - 1) / (16 * T)) : 0, each = (all_tiles + a.splits - 1) / a.splits;
   const int begin = min(split * each, all_tiles), tiles = min(begin + each, all_tiles) - begin;  // this range's
   const int32_t* const table = a.b.table + (int64_t)s * a.b.table_stride;
 
   Subtile sub = no_subtile();  // a lane knows one subtile of the next 64
+  uint64_t partly = 0;         // those that not all of the workgroup's rows see whole
   const auto look_up = [&](int tile) {
-    const int64_t at = (int64_t)lo + 16 * ((int64_t)4 * (begin + tile) + lane);
+    const int64_t at = (int64_t)lo + 16 * ((int64_t)T * (begin + tile) + lane);
     sub = no_subtile();
     if (at < hi) sub = find_subtile(a.c, table, a.b.width, h, (int)(at >> a.c.log2_page), (int)at & ((1 << a.c.log2_page) - 1));
+    partly = __builtin_amdgcn_ballot_w64(sub.pos + 15 > pos_lo || (int64_t)sub.pos <= (int64_t)pos_hi - a.window);
+    sub.ks *= a.scale2;
   };
-  // a lane's part of the next tile: wavefronts 0..3 values, 4..7 keys, of subtile wave % 4
-  uint32_t raw[8 * VW > 4 * KL ? 8 * VW : 4 * KL];
+  const auto place = [&](int tile, int u) { return (tile & (64 / T - 1)) * T + u; };  // the lane that knows subtile u
+  // a lane's part of the next tile: wavefronts 0..3 values, 4..7 keys, of SW subtiles
+  uint32_t raw[(8 * VW * VQ > 4 * KL * SW ? 8 * VW * VQ : 4 * KL * SW)];
   const bool has_values = wave < 4;
   const int dq = D == 64 ? r & 15 : r;
   const auto fetch = [&](int tile) {
-    const int at = __builtin_amdgcn_readlane(sub.at, ((tile & 15) << 2) + (wave & 3));
-    const int64_t off = (int64_t)(at < 0 ? 0 : at) * (16 * D);
+    int64_t off[SW];
+#pragma unroll
+    for (int q = 0; q < SW; ++q) off[q] = (int64_t)max(__builtin_amdgcn_readlane(sub.at, place(tile, SW * (wave & 3) + q)), 0) * (16 * D);
     if (has_values) {
-      if (D != 64 || r < 16) {
-        const uint8_t* const p = a.c.v + off + 4 * VW * dq;
+#pragma unroll
+      for (int q = 0; q < VQ; ++q) {
+        const uint8_t* const p = a.c.v + (D != 64 || r < 16 ? off[q] : off[SW - 1]) + 4 * VW * dq;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const uint8_t* const from = p + (4 * b + (j & 3) + (j >> 2) * 8) * D;
           if constexpr (VW == 1) {
-            raw[j] = *reinterpret_cast<const uint32_t*>(from);
+            raw[8 * q + j] = *reinterpret_cast<const uint32_t*>(from);
           } else {
             const uint2_t two = *reinterpret_cast<const uint2_t*>(from);
             raw[j] = two[0], raw[8 + j] = two[1];
@@ -111,40 +129,50 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         }
       }
     } else {
-      const uint8_t* const p = a.c.k + off + 16 * lane;  // 16 keys of d bytes in one piece
 #pragma unroll
-      for (int j = 0; j < KL; ++j) *reinterpret_cast<uint4_t*>(&raw[4 * j]) = *reinterpret_cast<const uint4_t*>(p + 1024 * j);
+      for (int q = 0; q < SW; ++q) {
+        const uint8_t* const p = a.c.k + off[q] + 16 * lane;  // 16 keys of d bytes in one piece
+#pragma unroll
+        for (int j = 0; j < KL; ++j) *reinterpret_cast<uint4_t*>(&raw[4 * (KL * q + j)]) = *reinterpret_cast<const uint4_t*>(p + 1024 * j);
+      }
     }
   };
   const auto put = [&](int half, bool masked) {
-    const int sb = wave & 3;
     if (has_values) {
-      if (CT == kPageE4m3 && masked) {
-        uint32_t flags = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t n = 0;
-          if (D != 64 || r < 16)
+      for (int q = 0; q < VQ; ++q) {
+        const int sb = SW * (wave & 3) + (D == 64 ? r >> 4 : q);
+        if (CT == kPageE4m3 && masked) {
+          uint32_t flags[SW] = {};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t n = 0;
 #pragma unroll
             for (int v = 0; v < VW; ++v) {
-              const uint32_t bytes = nan_bytes(raw[8 * v + j]);
-              raw[8 * v + j] &= ~bytes;
+              const uint32_t bytes = nan_bytes(raw[8 * (VW * q + v) + j]);
+              raw[8 * (VW * q + v) + j] &= ~bytes;
               n |= bytes;
             }
-          const uint64_t lanes = __builtin_amdgcn_ballot_w64(n != 0);
-          const int key = (j & 3) + (j >> 2) * 8;
-          flags |= ((uint32_t)lanes != 0 ? 1u << key : 0u) | ((uint32_t)(lanes >> 32) != 0 ? 16u << key : 0u);
+            const uint64_t lanes = __builtin_amdgcn_ballot_w64(n != 0);
+            const int key = (j & 3) + (j >> 2) * 8;
+#pragma unroll
+            for (int u = 0; u < (D == 64 ? SW : 1); ++u) {
+              const uint32_t half_of = D == 64 ? 0xffffu << 16 * u : 0xffffffffu;
+              flags[u] |= ((uint32_t)lanes & half_of) != 0 ? 1u << key : 0u;
+              flags[u] |= ((uint32_t)(lanes >> 32) & half_of) != 0 ? 16u << key : 0u;
+            }
+          }
+          if (lane == 0)
+#pragma unroll
+            for (int u = 0; u < (D == 64 ? SW : 1); ++u) poison_s[half][SW * (wave & 3) + q + u] = (uint16_t)flags[u];
         }
-        if (lane == 0) poison_s[half][sb] = (uint16_t)flags;
-      }
-      if (D != 64 || r < 16) {
         uint4_t* const to = lds + (2 * half + 1) * TILE + sb * (DA * 64) + 32 * b;
 #pragma unroll
         for (int v = 0; v < VW; ++v) {
           uint32_t turned[2][4];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const uint32_t *const w = raw + 8 * v + 4 * u;
+            const uint32_t *const w = raw + 8 * (VW * q + v) + 4 * u;
             const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
             const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
             turned[u][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
@@ -155,7 +183,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint4_t f = __builtin_bit_cast(uint4_t, codes_fp16<CT>(turned[0][e], turned[1][e]));
-            // coordinate 4 VW dq + 4 v + e = (d / 32) i + T
+            // coordinate 4 VW dq + 4 v + e = (d / 32) i + t
             if constexpr (D == 64) to[(e & 1) * 64 + 2 * dq + (e >> 1)] = f;
             else to[(4 * v + e) * 64 + dq] = f;
           }
@@ -164,19 +192,16 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     } else {
       uint4_t* const to = lds + 2 * half * TILE;
 #pragma unroll
-      for (int j = 0; j < KL; ++j) {
-        // bytes [16 lane + 1024 j, + 16) of the subtile: key, and 16 of its coordinates
-        const int byte = 16 * lane + 1024 * j, key = 16 * sb + byte / D, step = byte % D / 16;
-        union {
-          bf16x8_t v;
-          uint4_t w;
-        } f0, f1;
-        f0.v = codes_bf16<CT>(raw[4 * j], raw[4 * j + 1]);
-        f1.v = codes_bf16<CT>(raw[4 * j + 2], raw[4 * j + 3]);
-        uint4_t* const at = to + ((key >> 5) * KS + step) * 64;
-        at[(key & 31) ^ (step & 7)] = f0.w;
-        at[(32 + (key & 31)) ^ (step & 7)] = f1.w;
-      }
+      for (int q = 0; q < SW; ++q)
+#pragma unroll
+        for (int j = 0; j < KL; ++j) {
+          // bytes [16 lane + 1024 j, + 16) of the subtile: key, and 16 of its coordinates
+          const int byte = 16 * lane + 1024 * j, key = 16 * (SW * (wave & 3) + q) + byte / D, step = byte % D / 16;
+          const uint32_t* const w = raw + 4 * (KL * q + j);
+          uint4_t* const at = to + ((key >> 5) * KS + step) * 64;
+          at[(key & 31) ^ (step & 7)] = __builtin_bit_cast(uint4_t, codes_bf16<CT>(w[0], w[1]));
+          at[(32 + (key & 31)) ^ (step & 7)] = __builtin_bit_cast(uint4_t, codes_bf16<CT>(w[2], w[3]));
+        }
     }
   };
 
@@ -187,18 +212,13 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   float l = 0.f, M = -INFINITY, shift = 0.f, limit = -3e38f;
 
-  // where not all of the workgroup's rows see all of a tile: its subtiles' positions from the lanes that know them
-  const auto tile_pos = [&](int tile, int u) { return __builtin_amdgcn_readlane(sub.pos, ((tile & 15) << 2) + u); };
-  const auto is_masked = [&](int tile) {
-    const int p0 = tile_pos(tile, 0), p1 = tile_pos(tile, 1), p2 = tile_pos(tile, 2), p3 = tile_pos(tile, 3);
-    return max(max(p0, p1), max(p2, p3)) + 15 > pos_lo || (int64_t)min(min(p0, p1), min(p2, p3)) <= (int64_t)pos_hi - a.window;
-  };
+  const auto is_masked = [&](int tile) { return ((partly >> place(tile, 0)) & ((1u << T) - 1)) != 0; };
 
-  const auto step = [&](int half, const int (&sp)[4], const float (&ks)[4], const float (&lv)[4], const float (&iv)[4], bool masked) {
+  const auto step = [&](int half, int tile, int tile_pos, const float (&ks)[T], const float (&lv)[T], const float (&iv)[T], bool masked) {
     const uint4_t* const keys = lds + 2 * half * TILE;
     const uint4_t* const values = keys + TILE;
     // Fragments are fetched a phase ahead of their products (a product takes 32 cycles, a fetch over 100), and the barriers keep them there
-    uint4_t kf[KC], vf[2 * DT];
+    uint4_t kf[KC], vf[DT];
     const auto fetch_keys = [&](int kt, int k0) {
 #pragma unroll
       for (int k = 0; k < KC; ++k) kf[k] = keys[(kt * KS + k0 + k) * 64 + (lane ^ ((k0 + k) & 7))];
@@ -206,7 +226,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     fetch_keys(0, 0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < T / 2; ++kt) {
       float16_t acc;
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[i] = 0.f;
@@ -218,17 +238,20 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int i = 0; i < 2 * DT; ++i) vf[i] = values[((2 * kt + i / DT) * DA + dh * DT + i % DT) * 64 + lane];
+      for (int i = 0; i < DT; ++i) vf[i] = values[((2 * kt + i / DT) * DA + dh * DT + i % DT) * 64 + lane];
       __builtin_amdgcn_sched_barrier(0);
       uint32_t hidden = 0;  // bit i: key 8 (i / 4) + 4 b + i % 4 is not seen
       if (masked) {
-        const bool inner = max(sp[2 * kt], sp[2 * kt + 1]) + 15 <= mine_lo && (int64_t)min(sp[2 * kt], sp[2 * kt + 1]) > (int64_t)mine_hi - a.window;
+        const int sp[2] = {__builtin_amdgcn_readlane(tile_pos, place(tile, 2 * kt)), __builtin_amdgcn_readlane(tile_pos, place(tile, 2 * kt + 1))};
+        const bool inner = max(sp[0], sp[1]) + 15 <= mine_lo && (int64_t)min(sp[0], sp[1]) > (int64_t)mine_hi - a.window;
         uint32_t poison = 0;
         if (CT == kPageE4m3) poison = (uint32_t)poison_s[half][2 * kt] | (uint32_t)poison_s[half][2 * kt + 1] << 16;
         if (!inner || poison != 0) {
+          int b4 = 4 * b;
+          asm volatile("" : "+v"(b4));  // (else sixteen positions are carried through the loop)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int in = 8 * (i >> 2) + 4 * b + (i & 3), key = sp[2 * kt + (i >> 3)] + (in & 15);
+            const int in = 8 * (i >> 2) + b4 + (i & 3), key = sp[i >> 3] + (in & 15);
             const bool seen = key <= pos && (int64_t)key > (int64_t)pos - a.window;
             hidden |= seen ? 0u : 1u << i;
             if (seen && ((poison >> in) & 1)) acc[i] = __builtin_nanf("");
@@ -239,7 +262,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
       const auto exponents = [&] {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float ch = ks[2 * kt + u] * a.scale2, add = lv[2 * kt + u] + shift;
+          const float ch = ks[2 * kt + u], add = lv[2 * kt + u] + shift;
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[8 * u + i] = fmaf(acc[8 * u + i], ch, add);
         }
@@ -259,13 +282,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         const float down = M == next || M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - next);
         if (next != -INFINITY) {
           M = next;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] += BASE - next - shift;
           shift = BASE - next;
           limit = BASE + HEAD;
         }
         l *= down;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= down;
-        exponents();
       }
       half8_t p[2];
 #pragma unroll
@@ -276,12 +300,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[t]), p[0], o[t], 0, 0, 0);
+      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[t]), p[0], o[t], 0, 0, 0), vf[t] = values[((2 * kt + 1) * DA + dh * DT + t) * 64 + lane];
       __builtin_amdgcn_sched_barrier(0);
-      if (kt == 0) fetch_keys(1, 0);
+      if (kt + 1 < T / 2) fetch_keys(kt + 1, 0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[DT + t]), p[1], o[t], 0, 0, 0);
+      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, vf[t]), p[1], o[t], 0, 0, 0);
     }
   };
 
@@ -292,21 +316,20 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     put(0, masked);
     __syncthreads();
     for (int n = 0; n < tiles; ++n) {
-      int sp[4];
-      float ks[4], lv[4], iv[4];
+      const int tile_pos = sub.pos;
+      float ks[T], lv[T], iv[T];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int from = ((n & 15) << 2) + u;
-        sp[u] = __builtin_amdgcn_readlane(sub.pos, from);
+      for (int u = 0; u < T; ++u) {
+        const int from = place(n, u);
         ks[u] = lane_value(sub.ks, from), lv[u] = lane_value(sub.lv, from), iv[u] = lane_value(sub.iv, from);
       }
       bool next_masked = false;
       if (n + 1 < tiles) {
-        if (((n + 1) & 15) == 0) look_up(n + 1);
+        if (place(n + 1, 0) == 0) look_up(n + 1);
         next_masked = is_masked(n + 1);
         fetch(n + 1);
       }
-      step(n & 1, sp, ks, lv, iv, masked);
+      step(n & 1, n, tile_pos, ks, lv, iv, masked);
       if (n + 1 < tiles) put((n + 1) & 1, next_masked);
       masked = next_masked;
       __syncthreads();
@@ -342,7 +365,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 
 template <int D, int CT>
 hipError_t launch(const PagesAttendArgs& a, hipStream_t s) {
-  constexpr int bytes = 2 * 2 * 64 * D * 2;
+  constexpr int bytes = 2 * 2 * 16 * kSubtiles<D> * D * 2;
   static LdsLimit limit;
   const void* const kernel = reinterpret_cast<const void*>(&pages_attend_prompt_kernel<D, CT>);
   const hipError_t e = raise_lds_limit(limit, kernel, bytes);
