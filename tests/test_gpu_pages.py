@@ -240,6 +240,35 @@ def test_what_a_row_does_not_see_does_not_reach_it(d, dtype, seqs, new):
     assert got[:, sees_v][..., 7].isnan().all() and sees_v.any() and sees_k.any()
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 40])
+def test_prompts_over_values_that_are_not_numbers(d, window):
+    """A NaN in one coordinate of one key's values, every place of a tile in turn: that coordinate of the rows that see it, and what other
+    rows have keeps its bits."""
+    rng = np.random.default_rng([43, d, window])
+    page, heads, seqs, new, n = 16, 8, 20, 70, 150
+    b = Batch(rng, [n] * seqs, [new] * seqs, page)
+    p = filled(rng, b, heads, d, "e4m3")
+    q = torch.from_numpy(rng.standard_normal((b.rows, heads, d)).astype(np.float32)).to(DEV, torch.bfloat16)
+
+    def run():
+        out = torch.empty_like(q)
+        tq.tq_pages_attend(p, q, *b.args(), 0.1, out, window=window)
+        return out.view(seqs, new, heads, d).float()
+
+    clean = run()
+    at = [(17 * s + 3) % n if s < 4 else n - 1 - 7 * s % 130 for s in range(seqs)]
+    for s in range(seqs):
+        p.v.view(torch.uint8)[b.table[s][at[s] // page], :, at[s] % page, s % d] = 0x7f if s % 2 else 0xff
+    got = run()
+    pos = torch.arange(n - new, n, device=DEV)
+    for s in range(seqs):
+        sees = (pos >= at[s]) & ((pos - at[s] < window) if window else True)
+        assert torch.equal(got[s][~sees], clean[s][~sees]), s
+        assert got[s][sees][..., s % d].isnan().all(), s
+    assert sees.any()
+
+
 @pytest.mark.parametrize("d,page,kind,dtype,group,lens,new,n", [
     (128, 64, "e4m3", "bf16", 4, [700, 90], [1, 1], 5), (64, 16, "int8", "f32", 3, [300, 33], [4, 2], 9),
     (256, 32, "e4m3", "f32", 20, [200], [2], 1), (128, 16, "int8", "bf16", 16, [999], [3], 40),

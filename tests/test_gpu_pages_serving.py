@@ -357,3 +357,27 @@ def test_tables_lengths_and_starts_of_any_value(seed):
             tq.tq_pages_copy(p, put(wild(1, n_pages)), put(wild(1, n_pages)))
             torch.cuda.synchronize()
             assert all(ok() for ok in checks)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_prompts_of_any_tables_lengths_and_starts(d):
+    """The same for the kernel that takes many rows."""
+    rng = np.random.default_rng([71, d])
+    heads, page, n_pages, seqs, width, rows, most = 8, 16, 40, 32, 30, 900, 100
+    p = tq.make_pages(n_pages, heads, d, page, device=DEV)
+    p.k.copy_(torch.from_numpy(rng.integers(-100, 100, p.k.shape)).to(torch.int8).view(p.k.dtype))
+    p.v.copy_(torch.from_numpy(rng.integers(-100, 100, p.v.shape)).to(torch.int8).view(p.v.dtype))
+    p.k_scale.fill_(2.0**-6), p.v_scale.fill_(2.0**-6)
+    for k in range(4):
+        def wild(shape, near):
+            x = rng.integers(-2, near + 2, shape)
+            return np.where(rng.random(shape) < 0.2, rng.integers(-2**31, 2**31 - 1, shape), x)
+
+        starts = np.sort(wild(seqs + 1, rows)) if k % 2 else wild(seqs + 1, rows)
+        table, lens, starts = (torch.from_numpy(x).to(DEV, torch.int32) for x in (wild((seqs, width), n_pages), wild(seqs, width * page), starts))
+        q = torch.randn((rows, heads, d), device=DEV).to(torch.bfloat16)
+        raw, raw_lse = torch.full((rows + 8, heads, d), 5.0, device=DEV, dtype=torch.bfloat16), torch.full((rows + 8, heads), 5.0, device=DEV)
+        for window in (0, 70):
+            tq.tq_pages_attend(p, q, table, lens, starts, most, 0.1, raw[4:-4], lse=raw_lse[4:-4], window=window)
+        torch.cuda.synchronize()
+        assert all(bool((x[:4] == 5.0).all() and (x[-4:] == 5.0).all()) for x in (raw, raw_lse))
