@@ -504,25 +504,29 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   if (rows > 16 && !f32 && d == 128 && pages_attend_units(b, heads, group, chosen, 1) * keys >= 2048ll * device_cu_count()) plan.tiles = 2;
   const int64_t units = pages_attend_units(b, heads, group, chosen, plan.tiles);
   if (units == 0) return plan;
-  // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys until every compute unit has a
-  // workgroup, and taken where half of them (d = 256: three quarters) have one.
+  // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys, as many as give no
+  // compute unit a second workgroup, and taken where half of them (d = 256: three quarters) have one.
   // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 920 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
   // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577;
   // d = 256, where a workgroup has 128 rows: 427 of 1191 129 / 153, 500 of 1000 72 / 64
   const int64_t block = pages_prompt_rows(d), blocks = (int64_t)b.n_seqs * heads * ((rows + block - 1) / block);
   if (!chosen && !f32 && rows > 64) {
-    const int64_t fill = (device_cu_count() + blocks - 1) / blocks, most = (keys + 1023) / 1024;
+    const int64_t fill = device_cu_count() / blocks, most = (keys + 1023) / 1024;
     plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)16);
     plan.prompt = (d == 256 ? 4 : 6) * blocks * plan.splits >= 3 * device_cu_count();
     if (plan.prompt) return plan;
   }
-  // a workgroup for every compute unit, no more ranges than there are tiles for their wavefronts.  One token of 8 x 4 heads after
-  // 65536, us by workgroups: 128 43.1, 256 34.1, 512 34.8; four after 64 chosen pages: 16.8, 14.9, 15.2; 64 tokens after up to 8192 each
-  // 125 with 512 or 1024.  Up to six tiles to a wavefront the second launch costs more than it saves (8 x 4 heads, 200 / 512 / 700 tokens in one
-  // range 6.6 / 8.2 / 9.0, in more 10.1 / 9.7 / 9.9)
-  if (keys <= (d == 256 ? 512 : 768)) return plan;
-  const int64_t fill = (device_cu_count() + units - 1) / units, most = (keys + 32 * WAVES - 1) / (32 * WAVES);
-  plan.splits = (int)std::min(std::max(std::min(fill, most), (int64_t)1), (int64_t)64);
+  // As many ranges as give no compute unit a second workgroup while others have one (us by workgroups, 8 x 4 heads: 5 sequences of 8000
+  // tokens 240 20.6, 280 24.3; 12 sequences 192 38.8, 288 44.2; 9 of 4000, d = 256, 216 31.0, 288 43.7).  Twice that where it fills
+  // the card much better (20 sequences of 8000: 160 74, 320 73, 480 59) and for d = 64, whose workgroups need half the registers and have
+  // half the bytes on their way (14 of 4000: 224 18.5, 448 16.3; 24: 192 25.4, 384 23.0).
+  const int64_t cus = device_cu_count(), once = std::max(cus / units, (int64_t)1), twice = std::max(2 * cus / units, (int64_t)1);
+  int64_t splits = once;
+  if (d == 64 ? keys >= 512 * twice : d == 128 && plan.tiles == 1 && keys >= 1024 * twice && 8 * once < 3 * twice) splits = twice;
+  splits = std::min(std::min(splits, (keys + 32 * WAVES - 1) / (32 * WAVES)), (int64_t)64);  // (no more than there are tiles for their wavefronts)
+  // The second launch has to be earned (one range / many, 8 x 4 heads: one token after 512 8.2 / 9.3, 768 9.6 / 9.2; 16 sequences, two
+  // ranges, 1150 13.8 / 13.7, 1400 15.6 / 15.4; d = 256 384 9.7 / 10.4, 448 11.1 / 10.6)
+  plan.splits = splits > 1 && keys * (splits - 1) > (d == 256 ? 320 : 640) * splits ? (int)splits : 1;
   return plan;
 }
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits) {
