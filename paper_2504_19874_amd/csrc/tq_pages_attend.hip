@@ -506,7 +506,7 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   if (units == 0) return plan;
   // Prompts.  The kernel for them shares a tile between 256 rows; ranges of no fewer than 1024 keys, as many as give no
   // compute unit a second workgroup, and taken where half of them (d = 256: three quarters) have one.
-  // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 920 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
+  // us there / in the kernel below (8 x 4 heads, d = 128): 4 x 2048 new tokens of 8192 930 / 2506, 512 of 4096 64 / 98, 128 of 4096 34 / 34, 512
   // of 512 24 / 22; 64 sequences of 4096 with 8 new tokens each (32 rows) 264 / 121, 16 (64 rows) 263 / 205, 32 279 / 577;
   // d = 256, where a workgroup has 128 rows: 427 of 1191 129 / 153, 500 of 1000 72 / 64
   const int64_t block = pages_prompt_rows(d), blocks = (int64_t)b.n_seqs * heads * ((rows + block - 1) / block);
