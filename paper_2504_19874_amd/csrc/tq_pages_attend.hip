@@ -521,10 +521,11 @@ PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads
   // more than two: for d = 64, whose workgroups need half the registers and have half the bytes on their way (14 of 4000: 224 18.5, 448
   // 16.3; 24: 192 25.4, 384 23.0), and for few long ranges, where that fills the card better (20 of 8000: 160 74, 480 59) or evens out
   // lengths that differ (12, 14, 24 of 1000-8000: 192 37.0, 480 32.5; 224 37.1, 448 29.4; 192 60.0, 384 49.7; all of 8000: 37.8, 36.7; 39.3, 40.4;
-  // 76.7, 81.9).
-  const int64_t cus = device_cu_count(), once = std::max(cus / units, (int64_t)1), twice = std::max(2 * cus / units, (int64_t)1);
+  // 76.7, 81.9).  And as many as give them four where one range is more than one workgroup each and much less than two (36 sequences of 8000:
+  // 288 138, 864 118, of 1000-8000 95, 81; d = 256 278, 231).
+  const int64_t cus = device_cu_count(), once = std::max(cus / units, (int64_t)1), twice = std::max((units > cus && 4 * units < 7 * cus ? 4 : 2) * cus / units, (int64_t)1);
   int64_t splits = once;
-  if (d == 64 ? keys >= 512 * twice : d == 128 && plan.tiles == 1 && once < 4 && keys >= (twice == 2 ? 1536 : 1024) * twice) splits = twice;
+  if (d == 64 ? keys >= 512 * twice : once < 4 && (units > cus || (d == 128 && plan.tiles == 1)) && keys >= (twice == 2 ? 1536 : 1024) * twice) splits = twice;
   splits = std::min(std::min(splits, (keys + 32 * WAVES - 1) / (32 * WAVES)), (int64_t)64);  // (no more than there are tiles for their wavefronts)
   // The second launch has to be earned (one range / many, 8 x 4 heads: one token after 512 8.2 / 9.3, 768 9.6 / 9.2; 16 sequences, two
   // ranges, 1150 13.8 / 13.7, 1400 15.6 / 15.4; d = 256 384 9.7 / 10.4, 448 11.1 / 10.6)
