@@ -88,6 +88,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
     q[k] = u.v;
   }
 
+  const bool busy = first + 32 * rows_of < rows;  // (without rows a wavefront only turns codes: 66 rows, 16 sequences of 2000, 44.8 -> 40.2 us)
   const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
   const int hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 128));
   const int lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~63;
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
         next_masked = is_masked(n + 1);
         fetch(n + 1);
       }
-      step(n & 1, n, tile_pos, ks, lv, iv, masked);
+      if (busy) step(n & 1, n, tile_pos, ks, lv, iv, masked);
       if (n + 1 < tiles) put((n + 1) & 1, next_masked);
       masked = next_masked;
       __syncthreads();
