@@ -589,6 +589,8 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  * and not there (their entries stay -1).  Results do not depend on any order of execution.  n_pages <= 2^22 for these calls.
  *   tq_pages_reserve  every entry that is no page among those that hold the last max_new positions below lens[s] gets a
  *                     free page (refs = 1): to be called before an append, with lens already counting the new tokens.
+ *                     (n_seqs + 1024) times those of a sequence's width entries that max_new positions can lie in: below 2^31,
+ *                     else TQ_ERR_UNSUPPORTED.
  *   tq_pages_fork     row children[i] (lens 0, holding no pages) becomes a copy of row parents[i]: full pages are shared
  *                     (refs + 1), a last page that is not full is copied into a free one.  What is shared is not to
  *                     be appended to: a sequence is cut back (a smaller lens) no further than the pages of its own.  Skipped are a row outside

@@ -206,3 +206,9 @@ def test_attention_of_the_definition():
     assert np.allclose(po.attend(c, 16, q, [[2, 0, -1]], [20], [0, 3], 0.1, chosen=[[[1, -1]]] * 3)[0][2], 1.5)
     out, lse, *_ = po.attend(c, 16, q, [[-1, 5]], [20], [0, 3], 0.1)
     assert (out == 0).all() and np.isneginf(lse).all()
+
+
+def test_reserve_over_more_entries_than_it_counts(lib):
+    for more in (dict(n_seqs=1 << 21, max_new=2**31 - 1, width=4096, table_stride=4096), dict(n_seqs=2**31 - 1, max_new=1, width=1, table_stride=1),
+                 dict(n_seqs=1 << 30, max_new=129, width=2**31 - 1, table_stride=2**31 - 1)):
+        assert lib.tq_pages_reserve(C.byref(pages()), C.byref(batch(**more)), None, None) == UNSUPPORTED
