@@ -34,7 +34,7 @@ struct BatchView {
   __device__ __forceinline__ int count(int s) const { return starts != nullptr ? starts[s + 1] - starts[s] : max_new; }
 };
 
-// Numbers below 2^31 over one that the host knows: a product's upper half, a sum and a shift (scalar where the number is; the compiler's own
+// Numbers below 2^31 (2^31 + 2 for divisors below 2^30) over one that the host knows: a product's upper half, a sum and a shift (scalar where the number is; the compiler's own
 // division of two registers is some thirty vector instructions, of 64 bits over a hundred, in front of a kernel's first load).
 struct Divide {
   uint32_t mul, shift, by;
