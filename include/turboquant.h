@@ -496,7 +496,8 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *   Scales  tq_pages_append makes powers of two: the smallest 2^e with amax / 2^e <= 448 (127), e in [-40, 40], amax over
  *           the block's finite values; larger values (infinities among them) take the largest code, NaN takes NaN (int8: 0).
  *           A power of two lets a block whose scale grows be coded again without a second rounding of what stays
- *           representable.  tq_pages_attend takes any positive scales from 2^-40 to 2^40.
+ *           representable.  tq_pages_attend takes any positive scales from 2^-40 to 2^40; a scale of values that is no positive number
+ *           makes the rows that see its page NaN, and no others.
  *   Bounds  (optional) the smallest and largest value of every channel of a page's keys, rounded outward to bf16.
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.

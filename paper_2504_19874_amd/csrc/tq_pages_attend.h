@@ -119,6 +119,9 @@ __device__ __forceinline__ Subtile find_subtile(const PagesView& c, const int32_
   const float vs = c.v_scale[block];
   t.lv = __builtin_amdgcn_logf(vs);
   t.iv = 1.f / vs;
+  // A scale that is none (a page that nothing was appended to) makes the rows that see it NaN, by their logits: an unseen key has the
+  // weight 0, which must not meet 1 / 0 or NaN.
+  if (!(t.iv > 0.f && t.iv < INFINITY)) t.lv = __builtin_nanf(""), t.iv = 0.f;
   return t;
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
