@@ -1,7 +1,5 @@
 // Shared by the attention kernels over pages (tq_pages_attend.hip, tq_pages_attend_prompt.hip); the mathematics is described in the first.
 #pragma once
-#include <climits>
-
 #include "tq_pages.h"
 
 namespace tq {
@@ -99,22 +97,28 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
 }
 
+// Beyond every position that a row or a stored token has here: rows further on count as at the last one before it, and the tokens from it on
+// (fewer than 128 below 2^31) are not there.  What is no page lies at it, seen by no row; 127 above it is still an int.
+constexpr int NOWHERE = 0x7fffff80;
+__device__ __forceinline__ int row_position(int64_t at) { return (int)max(min(at, (int64_t)NOWHERE - 1), (int64_t)-1); }
+
 // One subtile of 16 keys, as a lane of a wavefront that looks up 64 at a time knows it.
 struct Subtile {
   int at;        // its place in the pool in units of 16 tokens, -1: its page is none
-  int pos;       // of its first token (far beyond every row where its page is none)
+  int pos;       // of its first token (NOWHERE where its page is none)
   float ks, lv, iv;  // scale of its keys, base-2 logarithm and inverse of that of its values
 };
-__device__ __forceinline__ Subtile no_subtile() { return Subtile{-1, 0x70000000, 1.f, 0.f, 1.f}; }
+__device__ __forceinline__ Subtile no_subtile() { return Subtile{-1, NOWHERE, 1.f, 0.f, 1.f}; }
 // the 16 tokens from position `off` of place i of a table's row on, head h
 __device__ __forceinline__ Subtile find_subtile(const PagesView& c, const int32_t* table, int width, int h, int i, int off) {
   Subtile t = no_subtile();
-  if (i < 0 || i >= width) return t;
+  const int64_t pos = ((int64_t)i << c.log2_page) + off;
+  if (i < 0 || i >= width || pos >= NOWHERE) return t;
   const int p = table[i];
   if (p < 0 || p >= c.n_pages) return t;
   const int64_t block = (int64_t)p * c.heads + h;
   t.at = (int)(((block << c.log2_page) + off) >> 4);
-  t.pos = (int)min(((int64_t)i << c.log2_page) + off, (int64_t)0x70000000);
+  t.pos = (int)pos;
   t.ks = c.k_scale[block];
   const float vs = c.v_scale[block];
   t.lv = __builtin_amdgcn_logf(vs);

@@ -28,7 +28,7 @@ namespace {
 template <int D>
 struct Tile {
   uint32_t k[2][D / 16], v[8][D / 64];
-  int pos[2];             // of the subtile's first token (far beyond every row where its page is none)
+  int pos[2];             // of the subtile's first token (NOWHERE where its page is none)
   float ks[2], lv[2], iv[2];  // scale of its keys, base-2 logarithm and inverse of that of its values
 };
 
@@ -81,14 +81,14 @@ struct Walk {
     if (first_row >= rows) return false;
     const int len = a.b.lens[s];
     row0 = a.b.first_row(s);
-    const int at0 = len - whole + t0;
-    pos_lo = at0 + token_of(first_row), pos_hi = at0 + token_of(min(first_row + 16 * R - 1, rows - 1));
+    const int64_t at0 = (int64_t)len - whole + t0;
+    pos_lo = row_position(at0 + token_of(first_row)), pos_hi = row_position(at0 + token_of(min(first_row + 16 * R - 1, rows - 1)));
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int m = min(first_row + 16 * i + r, rows - 1);
       const int64_t row = row_of(m);
       const bool there = first_row + 16 * i + r < rows && row >= 0 && row < a.b.n_rows;
-      pos[i] = at0 + token_of(m);
+      pos[i] = row_position(at0 + token_of(m));
       load_query(i, there, row * a.q.ld_row + head_of(m) * a.q.ld_head + g * (D / 4));
 #pragma unroll
       for (int e = 0; e < VE; ++e) o[i][e] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -97,9 +97,9 @@ struct Walk {
     const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
     lo = 0;
     if (a.chosen != nullptr) {
-      hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)INT_MAX - 64);
+      hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)NOWHERE);
     } else {
-      hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 64));
+      hi = (int)min((int64_t)pos_hi + 1, bound);
       lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
     }
     table = a.b.table + (int64_t)s * a.b.table_stride;

@@ -65,16 +65,17 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
   const int len = a.b.lens[s];
   const int64_t row0 = a.b.first_row(s);
   const auto token_of = [&](int m) { return (int)a.by_group.of((uint32_t)m); };
-  const int at0 = len - whole;
+  const int64_t at0 = (int64_t)len - whole;
 
   const int rows_of = kShare<D> == 1 ? wave : wave & 3, dh = kShare<D> == 1 ? 0 : wave >> 2;  // which 32 rows, which part of the coordinates
   const int m = min(first + 32 * rows_of + r, rows - 1);
   const int64_t row = row0 + token_of(m);
   const int head = h * group + m - token_of(m) * group;
   const bool there = first + 32 * rows_of + r < rows && row >= 0 && row < a.b.n_rows;
-  const int pos = at0 + token_of(m);
-  const int pos_lo = at0 + token_of(first), pos_hi = at0 + token_of(min(first + ROWS - 1, rows - 1));  // of the workgroup
-  const int mine_lo = at0 + token_of(min(first + 32 * rows_of, rows - 1)), mine_hi = at0 + token_of(min(first + 32 * rows_of + 31, rows - 1));
+  const auto position_of = [&](int m) { return row_position(at0 + token_of(m)); };
+  const int pos = position_of(m);
+  const int pos_lo = position_of(first), pos_hi = position_of(min(first + ROWS - 1, rows - 1));  // of the workgroup
+  const int mine_lo = position_of(min(first + 32 * rows_of, rows - 1)), mine_hi = position_of(min(first + 32 * rows_of + 31, rows - 1));
 
   bf16x8_t q[KS];
 #pragma unroll
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 
   const bool busy = first + 32 * rows_of < rows;  // (without rows a wavefront only turns codes: 66 rows, 16 sequences of 2000, 44.8 -> 40.2 us)
   const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
-  const int hi = (int)min((int64_t)pos_hi + 1, min(bound, (int64_t)INT_MAX - 128));
+  const int hi = (int)min((int64_t)pos_hi + 1, bound);
   const int lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~63;
   const int all_tiles = hi > lo ? (int)(((int64_t)hi - lo + 16 * T - 1) / (16 * T)) : 0, each = (all_tiles + a.splits - 1) / a.splits;
   const int begin = min(split * each, all_tiles), tiles = min(begin + each, all_tiles) - begin;  // this range's

@@ -64,8 +64,8 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
   const int whole = a.b.count(s);
   const int64_t row = a.b.first_row(s) + t;
   if (t >= whole || row < 0 || row >= a.b.n_rows) return;
-  const int pos = a.b.lens[s] - whole + t;
-  const int last = pos >= 0 ? pos >> a.c.log2_page : -1;
+  const int64_t pos = (int64_t)a.b.lens[s] - whole + t;
+  const int last = pos >= 0 ? (int)(pos >> a.c.log2_page) : -1;
   const int n = min(last + 1, a.b.width);
   // a wavefront: `steps` times 4 U pages
   const int first = (block * 4 + wave) * steps * (4 * U);
@@ -192,8 +192,8 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
   uint32_t held[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < a.b.width ? words[i * THREADS + tid] : 0u;
-  const int pos = a.b.lens[s] - whole + t;
-  const int n = pos >= 0 ? min((pos >> a.c.log2_page) + 1, a.b.width) : 0;
+  const int64_t pos = (int64_t)a.b.lens[s] - whole + t;
+  const int n = pos >= 0 ? min((int)(pos >> a.c.log2_page) + 1, a.b.width) : 0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) held[i] = i * THREADS + tid < n ? held[i] : 0u;  // (behind the row's last page nothing has been written)
   const auto each = [&](auto f) {

@@ -81,3 +81,49 @@ def test_a_scale_that_some_rows_see(d, dtype, seqs, new):
         sees = (torch.arange(n - new, n, device=DEV) >= n - page).repeat(seqs)
         assert torch.equal(got[0][~sees], want[0][~sees]) and torch.equal(got[1][~sees], want[1][~sees])
         assert got[0][sees].isnan().all() and got[1][sees].isnan().all()
+
+
+SHAPES = [(128, "bf16", 1, 3), (64, "f32", 2, 20), (256, "bf16", 1, 1), (64, "bf16", 24, 70), (128, "bf16", 24, 70), (256, "bf16", 24, 70)]
+
+
+@pytest.mark.parametrize("window", [0, 2**31 - 1, 9])
+@pytest.mark.parametrize("d,dtype,seqs,new", SHAPES)
+def test_the_largest_lengths_over_places_that_are_no_page(d, dtype, seqs, new, window):
+    """Lengths up to 2^31 - 1: what is no page is not there, whatever the pool's first tokens are; what is a page is seen whole."""
+    rng = np.random.default_rng([84, d, seqs])
+    heads, page = 8, 16
+    b = T.Batch(rng, [48] * seqs, [new] * seqs, page, spare=2, wide=0)
+    p = T.filled(rng, b, heads, d, "e4m3")
+    table, _, starts, most = b.args()
+    q = queries(rng, b.rows, heads, d, dtype)
+    none = torch.full_like(table, -1)
+    pick = ints([[[0, 1, 2]] * heads] * b.rows)
+    for n in (2**31 - 1, 2**31 - 1000, 0x70000000, 0x70000000 + new - 1):
+        lens = torch.full((seqs,), n, dtype=torch.int32, device=DEV)
+        for more in ({}, {"chosen": pick}):
+            out, lse = attended(p, q, none, lens, starts, most, window=window, **more)
+            assert (out == 0).all() and (lse == -math.inf).all(), n
+            holes = table.clone()
+            holes[:, 1] = -1
+            got = attended(p, q, holes, lens, starts, most, window=window, **more)
+            want = attended(p, q, holes, ints([1000] * seqs), starts, most, window=0 if window > 9 else window, **more)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), n
+
+
+@pytest.mark.parametrize("d,dtype,seqs,new", SHAPES)
+def test_the_smallest_lengths(d, dtype, seqs, new):
+    """Rows whose positions lie below -2^31 see nothing, and choose nothing."""
+    rng = np.random.default_rng([85, d, seqs])
+    heads, page = 8, 16
+    b = T.Batch(rng, [48] * seqs, [new] * seqs, page, spare=2, wide=0)
+    p = T.filled(rng, b, heads, d, "e4m3")
+    p = tq.Pages(p.k, p.v, p.k_scale, p.v_scale, bounds=torch.zeros((b.n_pages, heads, 2, d), dtype=torch.bfloat16, device=DEV))
+    table, _, starts, most = b.args()
+    q = queries(rng, b.rows, heads, d, dtype)
+    lens = torch.full((seqs,), -2**31, dtype=torch.int32, device=DEV)
+    for more in ({}, {"chosen": ints([[[0, 1, 2]] * heads] * b.rows)}):
+        out, lse = attended(p, q, table, lens, starts, most, **more)
+        assert (out == 0).all() and (lse == -math.inf).all()
+    chosen = torch.full((b.rows, heads, 3), 7, dtype=torch.int32, device=DEV)
+    tq.tq_pages_select(p, q, table, lens, starts, most, chosen)
+    assert (chosen == -1).all()
