@@ -574,9 +574,10 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
  * Choose pages for tq_pages_attend by their bounds.  For the row at position p and a head of the cache, page i (i up to
  * p / page_tokens) has the score
  *   max over the head's query heads of  sum_j max(q_j lower_ij, q_j upper_ij),
- * which no <q, k> of its keys exceeds; the sum is taken in 64 bits and rounded to fp32 once.  The first keep_first and the
- * last keep_last pages come first, then the others by score, equal scores by lower i, NaN last.  An entry of the table that
- * is no page is never chosen.
+ * which no <q, k> of its keys exceeds; the sum is taken in 64 bits and rounded to fp32 once.  A q_j of zero adds
+ * nothing, so that a bound may be infinite.  The first keep_first and the last keep_last pages come first, then the others by
+ * score, equal scores by lower i, NaN (of a query, a bound, or infinite terms of both signs) last.  An entry of the table that is
+ * no page is never chosen.
  *   chosen   device out [n_rows][n_heads][n_chosen]: the chosen pages' places in the table, ascending, then -1.
  * q as above.  n_chosen in [1, 1024], keep_first + keep_last <= n_chosen.  width <= 65536.  Uses c->workspace.
  */

@@ -127,12 +127,13 @@ def select(lower, upper, page, q, table, lens, starts, n_chosen, keep_first, kee
                     p = table[s][i]
                     if not 0 <= p < len(lower):
                         continue
-                    score = max((np.float32(np.sum(np.maximum(q[row, g] * lower[p, h], q[row, g] * upper[p, h]))) for g in
-                                 range(h * heads // kv, (h + 1) * heads // kv)))
-                    if i < keep_first or i > last - keep_last:
-                        score = np.float32(np.inf)
-                    rank.append((-score, i))
-                best = sorted(i for _, i in sorted(rank)[:n_chosen])
+                    with np.errstate(invalid="ignore", over="ignore"):
+                        x, lo, hi = q[row, h * heads // kv:(h + 1) * heads // kv], lower[p, h], upper[p, h]
+                        terms = np.where((x == 0) & ~np.isnan(lo) & ~np.isnan(hi), 0.0, np.maximum(x * lo, x * hi))
+                        score = terms.sum(1).astype(np.float32).max()  # (NaN of one head is the page's)
+                    kept = i < keep_first or i > last - keep_last
+                    rank.append((0, 0.0, i) if kept else (2, 0.0, i) if np.isnan(score) else (1, -score, i))
+                best = sorted(r[-1] for r in sorted(rank)[:n_chosen])
                 out[row, h, :len(best)] = best
     return out
 

@@ -84,6 +84,25 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
   };
   if (a.group <= G) stage(0);
 
+  // A page's sum as the definition has it, by one lane: the sum of two above has 0 * inf where the side that is not taken has no bound.
+  const auto defined = [&](int p, int g) {
+    const uint16_t* const from = a.c.bounds + ((int64_t)p * heads + h) * (2 * D);
+    double sum = 0.;
+    for (int c0 = 0; c0 < D && sum == sum; c0 += 8) {
+      const uint4_t low = *reinterpret_cast<const uint4_t*>(from + c0), high = *reinterpret_cast<const uint4_t*>(from + D + c0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = c0 + i;
+        const double x = q_s[g][c % C][c / C][0] + q_s[g][c % C][c / C][1];
+        const float l = __uint_as_float((i & 1) ? low[i >> 1] & 0xffff0000u : low[i >> 1] << 16);
+        const float u = __uint_as_float((i & 1) ? high[i >> 1] & 0xffff0000u : high[i >> 1] << 16);
+        if (x != x || l != l || u != u) sum = __builtin_nan("");
+        else if (x != 0.) sum = fma(x, (double)(x > 0. ? u : l), sum);
+      }
+    }
+    return (float)sum;
+  };
+
   for (int step = 0; step < steps; ++step) {
     const int base = first + step * (4 * U);
     bool there[U];
@@ -137,7 +156,11 @@ __global__ __launch_bounds__(256) void pages_score_kernel(const PagesSelectArgs 
       add_halves<2, XOR2, V / 4>(sum);
       add_halves<1, XOR1, V / 8>(sum);
       // lane j (of eight sums: lanes 2 i and 2 i + 1) has the sum of page sum / G of the lane group and head sum % G
-      const float v = (float)sum[0];
+      float v = (float)sum[0];
+      if (v != v) {
+        const int i = V == 16 ? j : j >> 1, place = base + 4 * (i / G) + lanes, p = place < n ? table[place] : -1;
+        if (p >= 0 && p < a.c.n_pages) v = defined(p, i % G);
+      }
       nan |= v != v;
       best = fmaxf(best, v);
     }
