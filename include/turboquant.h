@@ -539,6 +539,7 @@ typedef struct tq_batch {
 /*
  * Store the new keys and values.  k, v: device, n_rows rows (dtype TQ_F32 or TQ_BF16) of n_heads vectors, `ld_row` elements
  * between rows and `ld_head` between heads; 16-byte aligned, strides multiples of 16 bytes, else TQ_ERR_UNSUPPORTED.
+ * n_seqs times the pages that max_new tokens can lie in, width of them at most: below 2^24, else TQ_ERR_UNSUPPORTED.
  * A page whose first token is among the new ones starts afresh; in any other the scale grows to max(old, new) and the codes
  * that were there are rounded to it (an old one that is no power of two is first taken up to one).  Slots behind the last token stay as they were.  Two sequences of one call must not
  * store into the same page.  No workspace.
@@ -557,7 +558,10 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
  *   lse      device [n_rows][n_heads_q] fp32, or NULL.
  *   chosen   NULL: all tokens.  Else device [n_rows][n_heads][n_chosen]: places in the sequence's table (page i holds
  *            tokens [i * page_tokens, ..)) that the row's query heads read, in any order; entries outside [0, width) are
- *            skipped, one that is there twice counts twice.
+ *            skipped, one that is there twice counts twice.  n_chosen * page_tokens at most 2^31 - 128.
+ * n_seqs * max_new * n_heads_q below 2^31; n_seqs * n_heads times tiles of 16 rows (of max_new * n_heads_q / n_heads; where pages are
+ * chosen, n_seqs * max_new * n_heads times tiles of n_heads_q / n_heads) below 2^24, for prompts in bf16, 256 rows to a
+ * tile (d = 256: 128), below 2^23; else TQ_ERR_UNSUPPORTED.
  * Prompts and single tokens in one call share a plan made for the longest; in two calls each has its own.
  * Sums, maxima and weights are fp32.  Codes are exact factors in 16 bits; a bf16 query is one exact factor, an fp32 one
  * three; a softmax weight is taken in fp16 (bf16 output: relative error 2^-11, below the output's own half step 2^-8) or as
@@ -579,7 +583,9 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
  * score, equal scores by lower i, NaN (of a query, a bound, or infinite terms of both signs) last.  An entry of the table that is
  * no page is never chosen.
  *   chosen   device out [n_rows][n_heads][n_chosen]: the chosen pages' places in the table, ascending, then -1.
- * q as above.  n_chosen in [1, 1024], keep_first + keep_last <= n_chosen.  width <= 65536.  Uses c->workspace.
+ * q as above.  n_chosen in [1, 1024], keep_first + keep_last <= n_chosen.  width <= 65536.  n_seqs * max_new * n_heads
+ * below 2^24 (2^23, 2^22 where width is above 1024, 4096), and below 2^24 times 512 / width (one query head to a head of the
+ * cache: 1024 / width); else TQ_ERR_UNSUPPORTED.  Uses c->workspace.
  */
 size_t tq_pages_select_workspace_bytes(const tq_pages* c, const tq_batch* b);
 tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, int32_t dtype, int64_t ldq_row,
@@ -604,6 +610,7 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  *                     that holds pages must be in the batch.
  *   tq_pages_copy     page src[i] -> page dst[i] (device arrays of n pairs): codes, scales, bounds; not refs.  A page
  *                     that is copied to is in no other pair; a pair with a page outside [0, n_pages) is skipped.
+ * The lists of fork and free have fewer than 2^24 entries, else TQ_ERR_UNSUPPORTED.
  * Reserve, fork and compact use c->workspace: tq_pages_pool_workspace_bytes() (n: entries of a fork's lists, else 0).
  */
 size_t tq_pages_pool_workspace_bytes(const tq_pages* c, int64_t n);

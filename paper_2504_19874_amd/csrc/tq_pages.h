@@ -47,6 +47,9 @@ struct Divide {
   __device__ __forceinline__ uint32_t rest(uint32_t n, uint32_t quotient) const { return n - quotient * by; }
 };
 
+// One launch takes this many workgroups: it counts the threads of a dimension in 32 bits.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads <= 0xffffffffll; }
+
 // Rows of keys, values, queries or outputs.
 struct PagesRows {
   const void* p;
@@ -114,6 +117,7 @@ hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs&
 hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s);
 constexpr int pages_prompt_rows(int d) { return d == 256 ? 128 : 256; }  // to a workgroup
 
+// The launches below return hipErrorInvalidConfiguration, and have launched nothing, where a grid does not fit.
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,
                                hipStream_t s);
 
@@ -127,6 +131,7 @@ struct PagesSelectArgs {
   Divide by_heads, by_new, by_blocks;  // (blocks: workgroups that score the pages of a row and head)
 };
 hipError_t launch_pages_select(int d, bool f32, const PagesSelectArgs& a, hipStream_t s);
+bool pages_pick_fits(const BatchView& b, int heads);  // the grid of the choice itself
 
 hipError_t launch_pages_reserve(const PagesView& c, const BatchView& b, int32_t* list, int32_t* missing, hipStream_t s);
 hipError_t launch_pages_fork(const PagesView& c, const BatchView& b, int d, const int32_t* parents, const int32_t* children, int n, int32_t* list,

@@ -60,7 +60,8 @@ BatchView view(const tq_batch* b) {
   return v;
 }
 
-tq_status from_hip(hipError_t e) { return e == hipSuccess ? TQ_OK : TQ_ERR_HIP; }
+// (what a launch does not take is refused before any is made)
+tq_status from_hip(hipError_t e) { return e == hipSuccess ? TQ_OK : e == hipErrorInvalidConfiguration ? TQ_ERR_UNSUPPORTED : TQ_ERR_HIP; }
 
 // what attend, its workspace and select share
 tq_status check_queries(const tq_pages* c, const tq_batch* b, int32_t n_heads_q) {
@@ -72,7 +73,7 @@ tq_status check_queries(const tq_pages* c, const tq_batch* b, int32_t n_heads_q)
   return TQ_OK;
 }
 
-// a grid of `blocks` workgroups can be launched
+// products of sizes that the kernels hold in an int
 bool launchable(int64_t a, int64_t b, int64_t c) {
   const int64_t most = INT_MAX;
   return a <= most && b <= most && a * b <= most && c <= most && a * b * c <= most;
@@ -147,6 +148,7 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
   tq_status st = check_queries(c, b, n_heads_q);
   if (st != TQ_OK) return st;
   if ((dtype != TQ_F32 && dtype != TQ_BF16) || window < 0 || n_chosen < 0) return TQ_ERR_INVALID_ARG;
+  if (chosen != nullptr && (int64_t)n_chosen * c->page_tokens > INT_MAX - 127) return TQ_ERR_UNSUPPORTED;
   if (b->n_seqs == 0 || b->max_new == 0 || b->n_rows == 0) return TQ_OK;
   st = check_store(c);
   if (st != TQ_OK) return st;
@@ -173,6 +175,7 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
 
 size_t tq_pages_select_workspace_bytes(const tq_pages* c, const tq_batch* b) {
   if (check_pages(c) != TQ_OK || check_batch(b) != TQ_OK) return 0;
+  if (!launchable((int64_t)b->n_seqs * b->max_new, c->n_heads, 1) || !pages_pick_fits(view(b), c->n_heads)) return 0;
   return (size_t)b->n_rows * c->n_heads * b->width * sizeof(float);
 }
 
@@ -188,7 +191,7 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
   if (misaligned(c->bounds)) return TQ_ERR_UNSUPPORTED;
   st = check_rows(q, dtype, ldq_row, ldq_head, c->d);
   if (st != TQ_OK) return st;
-  if (!launchable((int64_t)b->n_seqs * b->max_new, c->n_heads, (b->width + 63) / 64)) return TQ_ERR_UNSUPPORTED;
+  if (!launchable((int64_t)b->n_seqs * b->max_new, c->n_heads, (b->width + 63) / 64) || !pages_pick_fits(view(b), c->n_heads)) return TQ_ERR_UNSUPPORTED;
   const size_t need = tq_pages_select_workspace_bytes(c, b);
   if (need > 0 && (c->workspace == nullptr || c->workspace_bytes < need || misaligned(c->workspace))) return TQ_ERR_WORKSPACE;
   PagesSelectArgs a;
@@ -217,6 +220,7 @@ tq_status tq_pages_fork(const tq_pages* c, const tq_batch* b, const int32_t* par
   if (b == nullptr || n < 0) return TQ_ERR_INVALID_ARG;
   tq_status st = check_pool(c, b, n);
   if (st != TQ_OK) return st;
+  if (!grid_fits(n, 256)) return TQ_ERR_UNSUPPORTED;
   if (n > 0 && (parents == nullptr || children == nullptr || !batch_arrays(b))) return TQ_ERR_INVALID_ARG;
   int32_t* const list = static_cast<int32_t*>(c->workspace);
   return from_hip(launch_pages_fork(view(c), view(b), c->d, parents, children, n, list, list + (c->n_pages + 1) / 2 * 2, missing, static_cast<hipStream_t>(stream)));
@@ -227,6 +231,7 @@ tq_status tq_pages_free(const tq_pages* c, const tq_batch* b, const int32_t* row
   tq_status st = check_pool(c, b, -1);
   if (st != TQ_OK) return st;
   if (n == 0) return TQ_OK;
+  if (!grid_fits(n, 256)) return TQ_ERR_UNSUPPORTED;
   if (rows == nullptr || !batch_arrays(b)) return TQ_ERR_INVALID_ARG;
   return from_hip(launch_pages_free(view(c), view(b), rows, n, static_cast<hipStream_t>(stream)));
 }

@@ -231,6 +231,7 @@ hipError_t launch(const PagesView& c, const BatchView& b, const PagesRows& k, co
   // max_new rows from any position on lie in no more than this many pages, and a sequence has no more than width
   int64_t pages_each = (((int64_t)b.max_new + (1 << c.log2_page) - 2) >> c.log2_page) + 1;
   if (pages_each > b.width) pages_each = b.width;
+  if (!grid_fits(b.n_seqs * pages_each, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)(b.n_seqs * pages_each), (unsigned)c.heads, 2);
   hipLaunchKernelGGL((pages_append_kernel<D, CT, F32, 256>), grid, dim3(256), 0, s, c, b, k, v, Divide(pages_each));
   return hipGetLastError();

@@ -97,7 +97,7 @@ struct Walk {
     const int64_t bound = (int64_t)a.b.width << a.c.log2_page;
     lo = 0;
     if (a.chosen != nullptr) {
-      hi = (int)min((int64_t)a.n_chosen << a.c.log2_page, (int64_t)NOWHERE);
+      hi = a.n_chosen << a.c.log2_page;  // (at most 2^31 - 128: tq_pages_attend)
     } else {
       hi = (int)min((int64_t)pos_hi + 1, bound);
       lo = (int)max((int64_t)0, (int64_t)pos_lo - a.window + 1) & ~31;
@@ -471,7 +471,9 @@ hipError_t launch(bool f32, PagesAttendArgs a, hipStream_t s) {
   if (a.prompt) {
     e = launch_pages_attend_prompt(D, CT, a, s);
   } else {
-    const dim3 grid((unsigned)(pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr, a.tiles) * a.splits));
+    const int64_t blocks = pages_attend_units(a.b, a.c.heads, a.group, a.chosen != nullptr, a.tiles) * a.splits;
+    if (!grid_fits(blocks, 64 * WAVES)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
     if (a.tiles == 2) {
       if constexpr (D == 128) hipLaunchKernelGGL((pages_attend_kernel<D, CT, false, 2>), grid, dim3(64 * WAVES), 0, s, a);
     } else {

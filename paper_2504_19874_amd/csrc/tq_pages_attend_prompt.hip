@@ -367,13 +367,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_attend_prompt_kernel(const P
 
 template <int D, int CT>
 hipError_t launch(const PagesAttendArgs& a, hipStream_t s) {
+  const int64_t row_tiles = ((int64_t)a.b.max_new * a.group + kRows<D> - 1) / kRows<D>, blocks = (int64_t)a.b.n_seqs * a.c.heads * row_tiles * a.splits;
+  if (!grid_fits(blocks, 64 * WAVES)) return hipErrorInvalidConfiguration;
   constexpr int bytes = 2 * 2 * 16 * kSubtiles<D> * D * 2;
   static LdsLimit limit;
   const void* const kernel = reinterpret_cast<const void*>(&pages_attend_prompt_kernel<D, CT>);
   const hipError_t e = raise_lds_limit(limit, kernel, bytes);
   if (e != hipSuccess) return e;
-  const int64_t row_tiles = ((int64_t)a.b.max_new * a.group + kRows<D> - 1) / kRows<D>;
-  hipLaunchKernelGGL((pages_attend_prompt_kernel<D, CT>), dim3((unsigned)((int64_t)a.b.n_seqs * a.c.heads * row_tiles * a.splits)), dim3(64 * WAVES), bytes, s, a);
+  hipLaunchKernelGGL((pages_attend_prompt_kernel<D, CT>), dim3((unsigned)blocks), dim3(64 * WAVES), bytes, s, a);
   return hipGetLastError();
 }
 

@@ -313,6 +313,9 @@ __global__ __launch_bounds__(THREADS) void pages_pick_kernel(const PagesSelectAr
   for (int i = above + min(equal, room) + tid; i < a.n_chosen; i += THREADS) out[i] = -1;
 }
 
+// of a workgroup that chooses from `width` pages
+int pick_threads(int width) { return width > 4096 ? 1024 : width > 1024 ? 512 : 256; }
+
 template <int D, bool F32, int G>
 hipError_t launch_score(PagesSelectArgs a, int64_t units, hipStream_t s) {
   // a wavefront takes a step (16 or 32 pages), up to eight where that leaves three workgroups for a compute unit.  Four rows of 8 heads and
@@ -322,6 +325,7 @@ hipError_t launch_score(PagesSelectArgs a, int64_t units, hipStream_t s) {
   int64_t steps = units * all / (3 * device_cu_count());
   steps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
   const int64_t blocks = (all + steps - 1) / steps;
+  if (!grid_fits(units * blocks, 256)) return hipErrorInvalidConfiguration;
   a.by_blocks = Divide(blocks);
   hipLaunchKernelGGL((pages_score_kernel<D, F32, G>), dim3((unsigned)(units * blocks)), dim3(256), 0, s, a, (int)steps);
   return hipGetLastError();
@@ -337,18 +341,22 @@ template <int D>
 hipError_t launch(bool f32, PagesSelectArgs a, hipStream_t s) {
   a.by_heads = Divide(a.c.heads), a.by_new = Divide(a.b.max_new);
   const int64_t units = (int64_t)a.b.n_seqs * a.b.max_new * a.c.heads;
+  if (!pages_pick_fits(a.b, a.c.heads)) return hipErrorInvalidConfiguration;
   if (a.b.width > 0) {
     const hipError_t e = f32 ? launch_score_g<D, true>(a, units, s) : launch_score_g<D, false>(a, units, s);
     if (e != hipSuccess) return e;
   }
   const dim3 grid((unsigned)units);
-  if (a.b.width > 4096) hipLaunchKernelGGL((pages_pick_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
-  else if (a.b.width > 1024) hipLaunchKernelGGL((pages_pick_kernel<512, 8>), grid, dim3(512), 0, s, a);
+  const int threads = pick_threads(a.b.width);
+  if (threads == 1024) hipLaunchKernelGGL((pages_pick_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
+  else if (threads == 512) hipLaunchKernelGGL((pages_pick_kernel<512, 8>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((pages_pick_kernel<256, 4>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+bool pages_pick_fits(const BatchView& b, int heads) { return grid_fits((int64_t)b.n_seqs * b.max_new * heads, pick_threads(b.width)); }
 
 hipError_t launch_pages_select(int d, bool f32, const PagesSelectArgs& a, hipStream_t s) {
   return d == 64 ? launch<64>(f32, a, s) : d == 128 ? launch<128>(f32, a, s) : launch<256>(f32, a, s);
