@@ -65,6 +65,12 @@ class TqBatch(C.Structure):
     ]
 
 
+class TqPagesCall(C.Structure):
+    """What the compiled half takes: a cache with the scratch memory of one thread's calls on one stream.  Not changed once it is made."""
+
+    _fields_ = [("c", TqPages), ("stream", C.c_uint64)]
+
+
 _P, _PG, _B = C.POINTER(TqParams), C.POINTER(TqPages), C.POINTER(TqBatch)
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 

@@ -237,19 +237,26 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// --- the paged cache: p.c (a tq_pages struct) and p.k, whose GPU every tensor is on and which is the current one ------------
+// --- the paged cache: its struct (p.c, or p._scratch.call where scratch memory is used) and p.k, whose GPU every tensor is on and which is
+// the current one -----------------------------------------------------------------------------------------------------------------
 
+// a cache with the scratch memory of the calling thread on one stream
+struct Call {
+  tq_pages c;
+  uint64_t stream;
+};
 struct Cache {
-  const tq_pages* c;
+  const tq_pages* c;  // the caller holds the struct for the length of the call, and nobody changes it
   c10::Device device;
 };
+template <class T = tq_pages>
 Cache cache(PyObject* const* o) {
   Py_buffer b;
   if (PyObject_GetBuffer(o[0], &b, PyBUF_SIMPLE) != 0) {
     PyErr_Clear();
     throw NotPlain{};
   }
-  const bool whole = (size_t)b.len == sizeof(tq_pages);
+  const bool whole = (size_t)b.len == sizeof(T);
   const tq_pages* c = static_cast<const tq_pages*>(b.buf);
   PyBuffer_Release(&b);
   const at::Tensor* k = tensor(o[1]);
@@ -304,6 +311,16 @@ Vectors vectors(const Cache& p, PyObject* o) {
 
 void* stream_of(const Cache& p) { return static_cast<void*>(c10::hip::getCurrentHIPStream(p.device.index()).stream()); }
 
+// the scratch memory is this stream's and large enough, and the call not captured (such a one has its own)
+void scratch(const Cache& p, size_t need, void* stream) {
+  if (need == 0) return;
+  const Call* const call = reinterpret_cast<const Call*>(p.c);
+  if (call->stream != (uint64_t)(uintptr_t)stream || p.c->workspace_bytes < need) throw NotPlain{};
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (stream != nullptr && (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) != hipSuccess || status != hipStreamCaptureStatusNone))
+    throw NotPlain{};
+}
+
 // p.c, p.k, k, v, table, lens, starts, max_new
 PyObject* pages_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 8, [&] {
@@ -327,10 +344,10 @@ int32_t* places(const Cache& p, PyObject* o, int64_t rows, int32_t* n) {
   return static_cast<int32_t*>(t.data_ptr());
 }
 
-// p.c, p.k, q, table, lens, starts, max_new, scale, out, lse, window, chosen
+// p._scratch.call, p.k, q, table, lens, starts, max_new, scale, out, lse, window, chosen
 PyObject* pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 12, [&] {
-    const Cache p = cache(a);
+    const Cache p = cache<Call>(a);
     const Vectors q = vectors(p, a[2]), out = vectors(p, a[8]);
     if (q.rows != out.rows || q.heads != out.heads || q.dtype != out.dtype || q.heads < 1 || q.heads % p.c->n_heads != 0 || q.rows < 1 ||
         (out.rows > 1 && out.ld_row == 0) || (out.heads > 1 && out.ld_head == 0) || !PyFloat_CheckExact(a[7]))
@@ -346,8 +363,8 @@ PyObject* pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t n_chosen;
     const int32_t* const chosen = places(p, a[11], q.rows, &n_chosen);
     const tq_batch b = batch(p, q.rows, a[3], a[4], a[5], integer32(a[6]));
-    if (p.c->workspace_bytes < tq_pages_attend_workspace_bytes(p.c, &b, (int32_t)q.heads, n_chosen, window)) throw NotPlain{};
     void* const s = stream_of(p);
+    scratch(p, tq_pages_attend_workspace_bytes(p.c, &b, (int32_t)q.heads, n_chosen, window), s);
     return unlocked([&] {
       return tq_pages_attend(p.c, &b, q.ptr, q.dtype, q.ld_row, q.ld_head, (int32_t)q.heads, scale, window, chosen, n_chosen, out.ptr, out.ld_row,
                              out.ld_head, lse, s);
@@ -355,52 +372,53 @@ PyObject* pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// p.c, p.k, q, table, lens, starts, max_new, chosen, keep_first, keep_last
+// p._scratch.call, p.k, q, table, lens, starts, max_new, chosen, keep_first, keep_last
 PyObject* pages_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 10, [&] {
-    const Cache p = cache(a);
+    const Cache p = cache<Call>(a);
     const Vectors q = vectors(p, a[2]);
     if (q.heads < 1 || q.heads % p.c->n_heads != 0 || q.rows < 1 || a[7] == Py_None || p.c->bounds == nullptr) throw NotPlain{};
     int32_t n_chosen;
     int32_t* const chosen = places(p, a[7], q.rows, &n_chosen);
     const tq_batch b = batch(p, q.rows, a[3], a[4], a[5], integer32(a[6]));
-    if (p.c->workspace_bytes < tq_pages_select_workspace_bytes(p.c, &b)) throw NotPlain{};
     const int32_t first = integer32(a[8]), last = integer32(a[9]);
     void* const s = stream_of(p);
+    scratch(p, tq_pages_select_workspace_bytes(p.c, &b), s);
     return unlocked([&] {
       return tq_pages_select(p.c, &b, q.ptr, q.dtype, q.ld_row, q.ld_head, (int32_t)q.heads, first, last, chosen, n_chosen, s);
     });
   });
 }
 
-void pool(const Cache& p, int64_t n) {
-  if (p.c->refs == nullptr || p.c->workspace_bytes < tq_pages_pool_workspace_bytes(p.c, n)) throw NotPlain{};
+void pool(const Cache& p, int64_t n, void* stream) {
+  if (p.c->refs == nullptr) throw NotPlain{};
+  scratch(p, tq_pages_pool_workspace_bytes(p.c, n), stream);
 }
 int32_t* one(const Cache& p, PyObject* o) { return o == Py_None ? nullptr : ints(p, o, 1); }
 
-// p.c, p.k, table, lens, max_new, missing
+// p._scratch.call, p.k, table, lens, max_new, missing
 PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 6, [&] {
-    const Cache p = cache(a);
-    pool(p, 0);
+    const Cache p = cache<Call>(a);
+    void* const s = stream_of(p);
+    pool(p, 0, s);
     const tq_batch b = batch(p, -1, a[2], a[3], Py_None, integer32(a[4]));
     int32_t* const missing = one(p, a[5]);
-    void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_reserve(p.c, &b, missing, s); });
   });
 }
 
-// p.c, p.k, table, lens, parents, children, missing
+// p._scratch.call, p.k, table, lens, parents, children, missing
 PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 7, [&] {
-    const Cache p = cache(a);
+    const Cache p = cache<Call>(a);
+    void* const s = stream_of(p);
     const int64_t forks = there(p, a[4], at::kInt, 1).size(0);
     if (forks > INT32_MAX) throw NotPlain{};
-    pool(p, forks);
+    pool(p, forks, s);
     const int32_t *const parents = ints(p, a[4], forks), *const children = ints(p, a[5], forks);
     const tq_batch b = batch(p, -1, a[2], a[3], Py_None, 0);
     int32_t* const missing = one(p, a[6]);
-    void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_fork(p.c, &b, parents, children, (int32_t)forks, missing, s); });
   });
 }
@@ -418,14 +436,14 @@ PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// p.c, p.k, table, n_live
+// p._scratch.call, p.k, table, n_live
 PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 4, [&] {
-    const Cache p = cache(a);
-    pool(p, 0);
+    const Cache p = cache<Call>(a);
+    void* const s = stream_of(p);
+    pool(p, 0, s);
     const tq_batch b = batch(p, -1, a[2], Py_None, Py_None, 0);
     int32_t* const live = one(p, a[3]);
-    void* const s = stream_of(p);
     return unlocked([&] { return tq_pages_compact(p.c, &b, live, s); });
   });
 }

@@ -3,11 +3,16 @@
 A batch is `table` (int32 [n_seqs][width]: the page that holds each span of a sequence's tokens), `lens` (int32 [n_seqs]: tokens
 of each sequence, those of the call among them), `starts` (int32 [n_seqs + 1]: where each sequence's rows begin in the call's
 arrays; None: every sequence has max_new rows) and `max_new` (at least the most rows of a sequence).  They stay on the GPU: nothing
-here waits for it, and every call can be captured into a graph once the workspace has its size (Pages.reserve_*).
+here waits for it, and every call can be captured into a graph (torch.cuda.graph).
+
+Scratch memory is the binding's: every thread has its own on every stream that it calls on, and a captured call has its own in the
+graph's memory.  So threads, streams and graphs may read one cache at the same time (tq_pages_attend, tq_pages_select); what writes to
+it (tq_pages_append and the pool's calls) the program puts in order with everything else, as for any tensor.
 """
 from __future__ import annotations
 
 import ctypes as C
+import threading
 
 import torch
 
@@ -20,6 +25,19 @@ _TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}
 def _where(t, what):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TurboQuantError(f"{what}: expected a GPU tensor")
+
+
+class _Scratch(threading.local):
+    """A thread's scratch memory of a cache: `spaces` by stream, and `call`, the struct with that of the stream it was used on last."""
+
+    def __init__(self, c):
+        self.spaces, self.call = {}, _lib.TqPagesCall(self.without(c), 0)
+
+    @staticmethod
+    def without(c):
+        c = _lib.TqPages.from_buffer_copy(c)
+        c.workspace, c.workspace_bytes = 0, 0
+        return c
 
 
 class Pages:
@@ -47,7 +65,7 @@ class Pages:
         self.k, self.v, self.k_scale, self.v_scale, self.bounds, self.refs = k, v, k_scale, v_scale, bounds, refs
         self.n_pages, self.n_heads, self.page_tokens, self.d = int(n), int(h), int(page), int(d)
         self.device = k.device
-        self.workspace, self._outgrown = None, []
+        self.workspace, self._reserved = None, []
         self.c = _lib.TqPages()
         self.c.d, self.c.n_heads, self.c.page_tokens, self.c.type, self.c.n_pages = self.d, self.n_heads, self.page_tokens, _TYPES[k.dtype], self.n_pages
         self.c.k, self.c.v = k.data_ptr(), v.data_ptr()
@@ -55,14 +73,39 @@ class Pages:
         self.c.bounds = 0 if bounds is None else bounds.data_ptr()
         self.c.refs = 0 if refs is None else refs.data_ptr()
         self.c.workspace, self.c.workspace_bytes = 0, 0
+        self._scratch = _Scratch(self.c)
+
+    def _with_scratch(self, need: int):
+        """-> the struct of a call that uses `need` bytes on the current stream (the cache's GPU is the current one), and what holds them
+        until the call has been made."""
+        if need == 0:
+            return _Scratch.without(self.c), None
+        if torch.cuda.is_current_stream_capturing():  # from the graph's memory, which stays the graph's
+            space = torch.empty(need, dtype=torch.uint8, device=self.device)
+            c = _Scratch.without(self.c)
+            c.workspace, c.workspace_bytes = space.data_ptr(), need
+            return c, space
+        mine, stream = self._scratch, torch.cuda.current_stream().cuda_stream
+        space = mine.spaces.get(stream)
+        have = 0 if space is None else space.numel()
+        if have < need:
+            # at least half as much again, for sizes that creep up; torch's allocator gives the old one away in the stream's order
+            space = mine.spaces[stream] = torch.empty(max(need, have + have // 2), dtype=torch.uint8, device=self.device)
+        if mine.call.stream != stream or mine.call.c.workspace != space.data_ptr():
+            c = _Scratch.without(self.c)
+            c.workspace, c.workspace_bytes = space.data_ptr(), space.numel()
+            mine.call = _lib.TqPagesCall(c, stream)
+        return mine.call.c, space
 
     def reserve_bytes(self, need: int):
-        """Make the device workspace at least `need` bytes.  One that it takes the place of is kept: a captured graph may hold its address."""
-        if need > self.c.workspace_bytes:
-            if self.workspace is not None:
-                self._outgrown.append(self.workspace)
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self.c.workspace, self.c.workspace_bytes = self.workspace.data_ptr(), need
+        """Make the calling thread's scratch memory on the current stream at least `need` bytes, so that no call there asks torch for more.
+        Calls of the C ABI with this object's struct (`c`) have it as their workspace; what an earlier one had stays theirs."""
+        if need > 0:
+            with torch.cuda.device(self.device):
+                c, space = self._with_scratch(need)
+            if need > self.c.workspace_bytes:
+                self._reserved.append(space)
+                self.workspace, self.c.workspace, self.c.workspace_bytes = space, c.workspace, c.workspace_bytes
         return self
 
     def reserve_attend(self, n_rows, n_seqs, width, n_heads_q, max_new=1, n_chosen=0, window=0):
@@ -75,7 +118,7 @@ class Pages:
         return self.reserve_bytes(int(_lib.load().tq_pages_select_workspace_bytes(C.byref(self.c), C.byref(b))))
 
     def reserve_pool(self, n: int = 0):
-        return self.reserve_bytes(int(_lib.load().tq_pages_pool_workspace_bytes(C.byref(self.c), n)))
+        return self.reserve_bytes(_pool_bytes(self, n))
 
 
 def make_pages(n_pages: int, n_heads: int, d: int, page_tokens: int, dtype=torch.float8_e4m3fn, bounds: bool = False, device="cuda") -> Pages:
@@ -132,10 +175,11 @@ def _writable(t, what):
         raise TurboQuantError(f"{what}: rows overlap")
 
 
-def _call(p: Pages, name: str, *args):
-    """One library call on the current stream of the cache's GPU."""
+def _call(p: Pages, name: str, *args, need: int = 0):
+    """One library call on the current stream of the cache's GPU, with `need` bytes of scratch memory."""
     with torch.cuda.device(p.device):
-        _check(getattr(_lib.load(), name)(C.byref(p.c), *args, C.c_void_p(torch.cuda.current_stream().cuda_stream)), name)
+        c, space = p._with_scratch(need)
+        _check(getattr(_lib.load(), name)(C.byref(c), *args, C.c_void_p(torch.cuda.current_stream().cuda_stream)), name)
 
 
 def _check_heads(n, p: Pages):
@@ -159,9 +203,8 @@ def tq_pages_append(p: Pages, k, v, table, lens, starts, max_new: int):
 
 
 def tq_pages_attend(p: Pages, q, table, lens, starts, max_new: int, scale: float, out, lse=None, window: int = 0, chosen=None):
-    """q, out [rows][n_heads_q][d]; lse float32 [rows][n_heads_q] or None; chosen int32 [rows][n_heads][n_chosen] or None.
-    Sizes the cache's workspace for the call when it is too small."""
-    st = _lib.call().pages_attend(p.c, p.k, q, table, lens, starts, max_new, scale, out, lse, window, chosen)
+    """q, out [rows][n_heads_q][d]; lse float32 [rows][n_heads_q] or None; chosen int32 [rows][n_heads][n_chosen] or None."""
+    st = _lib.call().pages_attend(p._scratch.call, p.k, q, table, lens, starts, max_new, scale, out, lse, window, chosen)
     if st is not None:
         return _check(st, "tq_pages_attend")
     pq, dtype, row, head = _rows(q, "q", p)
@@ -179,16 +222,16 @@ def tq_pages_attend(p: Pages, q, table, lens, starts, max_new: int, scale: float
         n_chosen = chosen.shape[-1] if chosen.dim() == 3 else 0
         _ints(chosen, "chosen", (n, p.n_heads, n_chosen), p.device)
     b = _batch(p, n, table, lens, starts, max_new)
-    p.reserve_bytes(int(_lib.load().tq_pages_attend_workspace_bytes(C.byref(p.c), C.byref(b), heads, n_chosen if chosen is not None else 0, window)))
+    need = int(_lib.load().tq_pages_attend_workspace_bytes(C.byref(p.c), C.byref(b), heads, n_chosen if chosen is not None else 0, window))
     # (an empty list is a list: its tensor may have no address)
     pc = None if chosen is None else C.c_void_p(chosen.data_ptr() or p.c.k)
     _call(p, "tq_pages_attend", C.byref(b), pq, dtype, row, head, heads, C.c_float(scale), window, pc, n_chosen, po, row_o, head_o,
-          None if lse is None else C.c_void_p(lse.data_ptr()))
+          None if lse is None else C.c_void_p(lse.data_ptr()), need=need)
 
 
 def tq_pages_select(p: Pages, q, table, lens, starts, max_new: int, chosen, keep_first: int = 1, keep_last: int = 1):
-    """chosen int32 [rows][n_heads][n_chosen] out.  Sizes the cache's workspace for the call when it is too small."""
-    st = _lib.call().pages_select(p.c, p.k, q, table, lens, starts, max_new, chosen, keep_first, keep_last)
+    """chosen int32 [rows][n_heads][n_chosen] out."""
+    st = _lib.call().pages_select(p._scratch.call, p.k, q, table, lens, starts, max_new, chosen, keep_first, keep_last)
     if st is not None:
         return _check(st, "tq_pages_select")
     pq, dtype, row, head = _rows(q, "q", p)
@@ -200,13 +243,17 @@ def tq_pages_select(p: Pages, q, table, lens, starts, max_new: int, chosen, keep
     if p.bounds is None:
         raise TurboQuantError("tq_pages_select: the cache has no bounds")
     b = _batch(p, n, table, lens, starts, max_new)
-    p.reserve_bytes(int(_lib.load().tq_pages_select_workspace_bytes(C.byref(p.c), C.byref(b))))
-    _call(p, "tq_pages_select", C.byref(b), pq, dtype, row, head, heads, keep_first, keep_last, C.c_void_p(pc), n_chosen)
+    need = int(_lib.load().tq_pages_select_workspace_bytes(C.byref(p.c), C.byref(b)))
+    _call(p, "tq_pages_select", C.byref(b), pq, dtype, row, head, heads, keep_first, keep_last, C.c_void_p(pc), n_chosen, need=need)
 
 
 def _pool(p: Pages):
     if p.refs is None:
         raise TurboQuantError("the cache has no reference counts")
+
+
+def _pool_bytes(p: Pages, n: int = 0):
+    return int(_lib.load().tq_pages_pool_workspace_bytes(C.byref(p.c), n))
 
 
 def _one(t, what, p: Pages):
@@ -215,26 +262,24 @@ def _one(t, what, p: Pages):
 
 def tq_pages_reserve(p: Pages, table, lens, max_new: int, missing=None):
     """Pages for the last max_new tokens of every sequence; missing int32 [1] out: pages that were not there."""
-    st = _lib.call().pages_reserve(p.c, p.k, table, lens, max_new, missing)
+    st = _lib.call().pages_reserve(p._scratch.call, p.k, table, lens, max_new, missing)
     if st is not None:
         return _check(st, "tq_pages_reserve")
     _pool(p)
     b = _batch(p, None, table, lens, None, max_new)
-    p.reserve_pool()
-    _call(p, "tq_pages_reserve", C.byref(b), _one(missing, "missing", p))
+    _call(p, "tq_pages_reserve", C.byref(b), _one(missing, "missing", p), need=_pool_bytes(p))
 
 
 def tq_pages_fork(p: Pages, table, lens, parents, children, missing=None):
     """Rows children[i] become copies of rows parents[i]."""
-    st = _lib.call().pages_fork(p.c, p.k, table, lens, parents, children, missing)
+    st = _lib.call().pages_fork(p._scratch.call, p.k, table, lens, parents, children, missing)
     if st is not None:
         return _check(st, "tq_pages_fork")
     _pool(p)
     n = int(parents.shape[0]) if isinstance(parents, torch.Tensor) and parents.dim() == 1 else -1
     pp, pc = _ints(parents, "parents", (n,), p.device), _ints(children, "children", (n,), p.device)
     b = _batch(p, None, table, lens, None, 0)
-    p.reserve_pool(n)
-    _call(p, "tq_pages_fork", C.byref(b), C.c_void_p(pp), C.c_void_p(pc), n, _one(missing, "missing", p))
+    _call(p, "tq_pages_fork", C.byref(b), C.c_void_p(pp), C.c_void_p(pc), n, _one(missing, "missing", p), need=_pool_bytes(p, n))
 
 
 def tq_pages_free(p: Pages, table, lens, rows):
@@ -251,13 +296,12 @@ def tq_pages_free(p: Pages, table, lens, rows):
 
 def tq_pages_compact(p: Pages, table, n_live=None):
     """The pages in use move to the front of the pool; n_live int32 [1] out."""
-    st = _lib.call().pages_compact(p.c, p.k, table, n_live)
+    st = _lib.call().pages_compact(p._scratch.call, p.k, table, n_live)
     if st is not None:
         return _check(st, "tq_pages_compact")
     _pool(p)
     b = _batch(p, None, table, None, None, 0)
-    p.reserve_pool()
-    _call(p, "tq_pages_compact", C.byref(b), _one(n_live, "n_live", p))
+    _call(p, "tq_pages_compact", C.byref(b), _one(n_live, "n_live", p), need=_pool_bytes(p))
 
 
 def tq_pages_copy(p: Pages, src, dst):
