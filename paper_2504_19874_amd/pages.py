@@ -12,6 +12,7 @@ it (tq_pages_append and the pool's calls) the program puts in order with everyth
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import threading
 
 import torch
@@ -139,6 +140,17 @@ def _ints(t, what, shape, device):
     return t.data_ptr()
 
 
+def _int32(x, what):
+    """(a ctypes argument would lose what lies above 32 bits)"""
+    try:
+        v = operator.index(x)
+    except TypeError:
+        raise TurboQuantError(f"{what}: expected a whole number, got {x!r}") from None
+    if not -2**31 <= v < 2**31:
+        raise TurboQuantError(f"{what}: {v} has more than 32 bits")
+    return v
+
+
 def _batch(p: Pages, n_rows, table, lens, starts, max_new: int):
     """n_rows None: a call without rows."""
     _where(table, "table")
@@ -147,6 +159,7 @@ def _batch(p: Pages, n_rows, table, lens, starts, max_new: int):
     n, width = table.shape
     if n > 1 and table.stride(0) < width:
         raise TurboQuantError("table: rows overlap")
+    max_new = _int32(max_new, "max_new")
     if max_new < 0 or (starts is None and n_rows is not None and n_rows < n * max_new):
         raise TurboQuantError(f"max_new: {n} sequences of {max_new} rows each, and {n_rows} rows")
     b = _lib.TqBatch()
@@ -221,7 +234,7 @@ def tq_pages_attend(p: Pages, q, table, lens, starts, max_new: int, scale: float
         _where(chosen, "chosen")
         n_chosen = chosen.shape[-1] if chosen.dim() == 3 else 0
         _ints(chosen, "chosen", (n, p.n_heads, n_chosen), p.device)
-    b = _batch(p, n, table, lens, starts, max_new)
+    b, window = _batch(p, n, table, lens, starts, max_new), _int32(window, "window")
     need = int(_lib.load().tq_pages_attend_workspace_bytes(C.byref(p.c), C.byref(b), heads, n_chosen if chosen is not None else 0, window))
     # (an empty list is a list: its tensor may have no address)
     pc = None if chosen is None else C.c_void_p(chosen.data_ptr() or p.c.k)
@@ -242,7 +255,7 @@ def tq_pages_select(p: Pages, q, table, lens, starts, max_new: int, chosen, keep
     pc = _ints(chosen, "chosen", (n, p.n_heads, n_chosen), p.device)
     if p.bounds is None:
         raise TurboQuantError("tq_pages_select: the cache has no bounds")
-    b = _batch(p, n, table, lens, starts, max_new)
+    b, keep_first, keep_last = _batch(p, n, table, lens, starts, max_new), _int32(keep_first, "keep_first"), _int32(keep_last, "keep_last")
     need = int(_lib.load().tq_pages_select_workspace_bytes(C.byref(p.c), C.byref(b)))
     _call(p, "tq_pages_select", C.byref(b), pq, dtype, row, head, heads, keep_first, keep_last, C.c_void_p(pc), n_chosen, need=need)
 
