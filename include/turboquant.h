@@ -596,8 +596,11 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  * The pool.  c->refs counts the table rows that hold a page; 0 is a free page.  Free pages are given out lowest first, in
  * the order of the rows (entries of the list); `missing` (device, nullable) is set to the number of pages that were wanted
  * and not there (their entries stay -1).  Results do not depend on any order of execution.  n_pages <= 2^22 for these calls.
- *   tq_pages_reserve  every entry that is no page among those that hold the last max_new positions below lens[s] gets a
- *                     free page (refs = 1): to be called before an append, with lens already counting the new tokens.
+ *   tq_pages_reserve  every entry that is no page among those that hold the call's new tokens of a sequence (b->starts, as for
+ *                     append; NULL: all of the last max_new positions below lens[s]) gets a free page (refs = 1): to be
+ *                     called before an append, with lens already counting the new tokens.  An entry that holds earlier
+ *                     tokens as well stays as it is and counts as missing: those had no page to be stored in, and a page
+ *                     that is given out holds what it held.
  *                     (n_seqs + 1024) times those of a sequence's width entries that max_new positions can lie in: below 2^31,
  *                     else TQ_ERR_UNSUPPORTED.
  *   tq_pages_fork     row children[i] (lens 0, holding no pages) becomes a copy of row parents[i]: full pages are shared

@@ -151,13 +151,16 @@ class Pool:
         self.refs[free[0]] = 1
         return int(free[0])
 
-    def reserve(self, max_new):
+    def reserve(self, max_new, starts=None):
         missing = 0
         for s in range(len(self.lens)):
-            for i in range(max(0, self.lens[s] - max_new) // self.page, -(-max(self.lens[s], 0) // self.page)):
-                if i < self.table.shape[1] and not 0 <= self.table[s, i] < len(self.refs):
-                    self.table[s, i] = self._take()
-                    missing += self.table[s, i] < 0
+            new = max_new if starts is None else min(max(starts[s + 1] - starts[s], 0), max_new)
+            first = max(0, self.lens[s] - new)
+            for i in range(first // self.page, -(-max(self.lens[s], 0) // self.page)):
+                if new > 0 and i < self.table.shape[1] and not 0 <= self.table[s, i] < len(self.refs):
+                    if i * self.page >= first:  # (else tokens before the new ones were there without a page)
+                        self.table[s, i] = self._take()
+                    missing += not 0 <= self.table[s, i] < len(self.refs)
         return missing
 
     def fork(self, parents, children):

@@ -45,22 +45,28 @@ __device__ __forceinline__ bool is_page(const PagesView& c, int p) { return p >=
 __global__ __launch_bounds__(THREADS) void pages_reserve_kernel(const PagesView c, const BatchView b, const Divide each, int32_t* list,
                                                                int32_t* missing) {
   __shared__ int wave_s[WAVES];
+  __shared__ int lost_s;  // entries that hold tokens before the new ones, which had no page to go to: a free one has somebody else's
   const uint32_t items = (uint32_t)b.n_seqs * each.by;
-  const auto entry = [&](uint32_t item) -> int32_t* {
+  const auto entry = [&](uint32_t item, bool count) -> int32_t* {
     if (item >= items) return nullptr;
     const uint32_t s = each.of(item);
-    const int64_t len = b.lens[s], from = len > b.max_new ? len - b.max_new : 0;
+    const int64_t len = b.lens[s], most = max(min(b.count((int)s), b.max_new), 0), from = len > most ? len - most : 0;
     const int64_t i = (from >> c.log2_page) + each.rest(item, s);
-    if ((i << c.log2_page) >= len || i >= b.width) return nullptr;
+    if (most == 0 || (i << c.log2_page) >= len || i >= b.width) return nullptr;
     int32_t* const e = b.table + (int64_t)s * b.table_stride + i;
-    return is_page(c, *e) ? nullptr : e;
+    if (is_page(c, *e)) return nullptr;
+    if ((i << c.log2_page) >= from) return e;
+    if (count) atomicAdd(&lost_s, 1);
+    return nullptr;
   };
+  if (threadIdx.x == 0) lost_s = 0;
+  __syncthreads();
   int want = 0;
-  for (uint32_t i = 0; i < items; i += THREADS) rank_of(entry(i + threadIdx.x) != nullptr, want, wave_s);
+  for (uint32_t i = 0; i < items; i += THREADS) rank_of(entry(i + threadIdx.x, true) != nullptr, want, wave_s);
   const int got = free_pages(c, want, list, wave_s);
   int at = 0;
   for (uint32_t i = 0; i < items; i += THREADS) {
-    int32_t* const e = entry(i + threadIdx.x);
+    int32_t* const e = entry(i + threadIdx.x, false);
     const int rank = rank_of(e != nullptr, at, wave_s);
     if (e != nullptr) {
       const int p = rank < got ? list[rank] : -1;
@@ -68,7 +74,7 @@ __global__ __launch_bounds__(THREADS) void pages_reserve_kernel(const PagesView 
       if (p >= 0) c.refs[p] = 1;
     }
   }
-  if (threadIdx.x == 0 && missing != nullptr) *missing = want - got;
+  if (threadIdx.x == 0 && missing != nullptr) *missing = want - got + lost_s;
 }
 
 // What fork i does, written by the first kernel for the second: the tokens of its parent (-1: it is skipped) and the free page that the

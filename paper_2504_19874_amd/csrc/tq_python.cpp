@@ -396,14 +396,14 @@ void pool(const Cache& p, int64_t n, void* stream) {
 }
 int32_t* one(const Cache& p, PyObject* o) { return o == Py_None ? nullptr : ints(p, o, 1); }
 
-// p._scratch.call, p.k, table, lens, max_new, missing
+// p._scratch.call, p.k, table, lens, starts, max_new, missing
 PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call(n, 6, [&] {
+  return call(n, 7, [&] {
     const Cache p = cache<Call>(a);
     void* const s = stream_of(p);
     pool(p, 0, s);
-    const tq_batch b = batch(p, -1, a[2], a[3], Py_None, integer32(a[4]));
-    int32_t* const missing = one(p, a[5]);
+    const tq_batch b = batch(p, -1, a[2], a[3], a[4], integer32(a[5]));
+    int32_t* const missing = one(p, a[6]);
     return unlocked([&] { return tq_pages_reserve(p.c, &b, missing, s); });
   });
 }

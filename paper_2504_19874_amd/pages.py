@@ -273,13 +273,13 @@ def _one(t, what, p: Pages):
     return None if t is None else C.c_void_p(_ints(t, what, (1,), p.device))
 
 
-def tq_pages_reserve(p: Pages, table, lens, max_new: int, missing=None):
-    """Pages for the last max_new tokens of every sequence; missing int32 [1] out: pages that were not there."""
-    st = _lib.call().pages_reserve(p._scratch.call, p.k, table, lens, max_new, missing)
+def tq_pages_reserve(p: Pages, table, lens, max_new: int, missing=None, starts=None):
+    """Pages for the new tokens of every sequence (without starts: the last max_new); missing int32 [1] out: pages that were not there."""
+    st = _lib.call().pages_reserve(p._scratch.call, p.k, table, lens, starts, max_new, missing)
     if st is not None:
         return _check(st, "tq_pages_reserve")
     _pool(p)
-    b = _batch(p, None, table, lens, None, max_new)
+    b = _batch(p, None, table, lens, starts, max_new)
     _call(p, "tq_pages_reserve", C.byref(b), _one(missing, "missing", p), need=_pool_bytes(p))
 
 
