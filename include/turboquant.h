@@ -498,7 +498,10 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *           A power of two lets a block whose scale grows be coded again without a second rounding of what stays
  *           representable.  tq_pages_attend takes any positive scales from 2^-40 to 2^40; a scale of values that is no positive number
  *           makes the rows that see its page NaN, and no others.
- *   Bounds  (optional) the smallest and largest value of every channel of a page's keys, rounded outward to bf16.
+ *   Bounds  (optional) the smallest and largest value of every channel of a page's keys as they were appended, rounded outward
+ *           to bf16.  A stored key may lie beyond them by its code's roundings: e4m3 by 2^-4 of the larger bound's magnitude and
+ *           2^-9 of the scale, int8 by the scale (half of it where the scale has not grown since).  A NaN bounds nothing, nor
+ *           does a value beyond the largest code of the largest scale, which is stored as that.
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
  *   lens[s] tokens of sequence s, the call's own new tokens among them: row j of its count rows is at position
@@ -578,7 +581,8 @@ tq_status tq_pages_attend(const tq_pages* c, const tq_batch* b, const void* q, i
  * Choose pages for tq_pages_attend by their bounds.  For the row at position p and a head of the cache, page i (i up to
  * p / page_tokens) has the score
  *   max over the head's query heads of  sum_j max(q_j lower_ij, q_j upper_ij),
- * which no <q, k> of its keys exceeds; the sum is taken in 64 bits and rounded to fp32 once.  A q_j of zero adds
+ * which no <q, k> of its keys as they were appended exceeds (one of a stored key may, by |q| times what Bounds above says);
+ * the sum is taken in 64 bits and rounded to fp32 once.  A q_j of zero adds
  * nothing, so that a bound may be infinite.  The first keep_first and the last keep_last pages come first, then the others by
  * score, equal scores by lower i, NaN (of a query, a bound, or infinite terms of both signs) last.  An entry of the table that is
  * no page is never chosen.

@@ -1,6 +1,7 @@
 // Choosing pages by the bounds of their keys.
 //
-// No key k of a page with bounds lo <= k <= hi has <q, k> above sum_j max(q_j lo_j, q_j hi_j).  The sums are taken in 64 bits (a
+// No key k with lo <= k <= hi has <q, k> above sum_j max(q_j lo_j, q_j hi_j): none of a page's keys as they were appended; their codes may lie
+// beyond by a rounding.  The sums are taken in 64 bits (a
 // product of two bf16 values is exact there, and so is the sum of a page's products unless they are 2^30 apart) and rounded to fp32
 // once: which page is chosen does not depend on the order of a sum.
 //

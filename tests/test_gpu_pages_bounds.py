@@ -46,3 +46,36 @@ def test_bounds_that_are_not_finite(d, page, dtype, heads, group, lens, new, n):
         tq.tq_pages_select(p, t, *b.args(), chosen, keep_first=0, keep_last=1)
         want = po.select(*[T.as64(bounds[:, :, i]) for i in (0, 1)], page, t.double().cpu().numpy(), b.table, b.lens, b.starts, n, 0, 1)
         assert np.array_equal(chosen.cpu().numpy(), want), case
+
+
+@pytest.mark.parametrize("kind,dtype", [("e4m3", "f32"), ("e4m3", "bf16"), ("int8", "f32")])
+def test_bounds_hold_what_was_appended_and_nearly_what_is_stored(kind, dtype):
+    """Keys appended a few at a time, larger and larger, so that codes are rounded again and again.  Every value lies between its channel's
+    bounds.  A stored one may lie beyond them: e4m3 by its first rounding, 2^-4 of its size, and by roundings to subnormal codes, half of
+    2^-9 of the scale that each is made with; int8 by half of the scale that each is made with.  A scale that grows at least doubles,
+    so the scales up to the last one add up to less than twice that.  The sum of a row's products is within that of the page's score."""
+    rng = np.random.default_rng([92, kind == "int8"])
+    heads, d, page = 2, 64, 16
+    p = tq.make_pages(1, heads, d, page, dtype=T.KINDS[kind], bounds=True, device=DEV)
+    x = rng.standard_normal((page, heads, d)) * np.exp2(np.linspace(0, 9, page))[:, None, None] * np.exp(rng.normal(0, 2, (page, heads, d)))
+    x = torch.from_numpy(x.astype(np.float32)).to(T.TYPES[dtype])
+    table, n, beyond = ints([[0]]), 0, 0
+    for new in (1, 1, 2, 1, 3, 1, 1, 4, 2):
+        part = x[n:n + new].to(DEV)
+        n += new
+        tq.tq_pages_append(p, part, part, table, ints([n]), None, new)
+        c = T.cache64(p)
+        lower, upper, scale = c["lower"][0], c["upper"][0], c["k_scale"][0][:, None]
+        given = x[:n].double().numpy().transpose(1, 0, 2)
+        stored = (c["k"][0] * scale[:, None])[:, :n]
+        assert (given >= lower[:, None]).all() and (given <= upper[:, None]).all()
+        excess = 2.0**-4 * np.maximum(np.abs(lower), np.abs(upper)) + 2.0**-9 * scale if kind == "e4m3" else np.broadcast_to(scale, lower.shape)
+        assert (stored >= (lower - excess)[:, None]).all() and (stored <= (upper + excess)[:, None]).all()
+        q = rng.standard_normal((20, d))
+        for h in range(heads):
+            score = np.maximum(q * lower[h], q * upper[h]).sum(1)
+            sums = 1e-12 * np.abs(q) @ np.maximum(np.abs(lower[h]), np.abs(upper[h]))  # (of the 64-bit sums here)
+            assert ((q @ given[h].T).max(1) <= score + sums).all()
+            assert ((q @ stored[h].T).max(1) <= score + np.abs(q) @ excess[h] + sums).all()
+        beyond += int((stored > upper[:, None]).sum() + (stored < lower[:, None]).sum())
+    assert n == page and beyond > 0
