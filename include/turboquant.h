@@ -607,7 +607,7 @@ tq_status tq_pages_select(const tq_pages* c, const tq_batch* b, const void* q, i
  *                     that is given out holds what it held.
  *                     (n_seqs + 1024) times those of a sequence's width entries that max_new positions can lie in: below 2^31,
  *                     else TQ_ERR_UNSUPPORTED.
- *   tq_pages_fork     row children[i] (lens 0, holding no pages) becomes a copy of row parents[i]: full pages are shared
+ *   tq_pages_fork     row children[i] (lens 0 or below, holding no pages) becomes a copy of row parents[i]: full pages are shared
  *                     (refs + 1), a last page that is not full is copied into a free one.  What is shared is not to
  *                     be appended to: a sequence is cut back (a smaller lens) no further than the pages of its own.  Skipped are a row outside
  *                     [0, n_seqs), a child that holds tokens (its parent itself too) or that an earlier entry has.

@@ -171,12 +171,12 @@ class Pool:
             skip.append(not (0 <= p < len(self.lens) and 0 <= c < len(self.lens)) or p == c or self.lens[c] > 0 or c in taken)
             if not skip[-1]:
                 taken.add(c)
-        before = self.lens.copy()
+        before = np.maximum(self.lens, 0)
         for n, (p, c) in enumerate(zip(parents, children)):  # pages are given out before any count changes
             if skip[n]:
                 continue
-            full = self.lens[p] // self.page
-            if self.lens[p] % self.page and full < self.table.shape[1] and 0 <= self.table[p, full] < len(self.refs):
+            full = before[p] // self.page
+            if before[p] % self.page and full < self.table.shape[1] and 0 <= self.table[p, full] < len(self.refs):
                 fresh[n] = self._take()
                 missing += fresh[n] < 0
                 if fresh[n] >= 0:

@@ -91,7 +91,10 @@ __global__ __launch_bounds__(THREADS) void pages_fork_kernel(const PagesView c, 
   for (int i = threadIdx.x; i < n; i += THREADS) {
     const int p = parents[i], s = children[i];
     forks[i] = Fork{-1, -1};
-    if (is_row(p) && is_row(s) && p != s && b.lens[s] <= 0) forks[i].len = max(b.lens[p], 0);
+    if (is_row(p) && is_row(s) && p != s && b.lens[s] <= 0) {
+      forks[i].len = max(b.lens[p], 0);
+      if (b.lens[s] != 0) b.lens[s] = 0;  // (a length below zero is none; it must not stand before an entry's number)
+    }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += THREADS)

@@ -68,6 +68,26 @@ def test_rows_of_different_counts():
         assert (table[2, 0].item() >= 0) == (page > 0)  # (without them all of the last 20 positions are new)
 
 
+def test_forks_into_rows_of_negative_lengths():
+    """They hold no tokens: the same as a length of zero, whatever its size beside the list's."""
+    rng = np.random.default_rng(122)
+    for below in (-1, -2, -3, -1000, -2**31):
+        p, pool = T.pool_state(rng, 40, 6, 4, 16, live=2)
+        pool.lens[:2], pool.table[:], pool.refs[:] = [20, 33], -1, 0
+        pool.table[0, :2], pool.table[1, :3], pool.refs[:5] = [0, 1], [2, 3, 4], 1
+        p.refs.copy_(ints(pool.refs))
+        pool.lens[2:5] = below
+        table, lens = ints(pool.table), ints(pool.lens)
+        parents, children = [0, 1, 0, 4, 1], [2, 3, 3, 5, 4]
+        want = T.contents(p)
+        pairs, short = pool.fork(parents, children)
+        missing = ints([-1])
+        tq.tq_pages_fork(p, table, lens, ints(parents), ints(children), missing=missing)
+        assert T.same_pool(p, pool, table, lens) and int(missing) == short, below
+        assert all(torch.equal(a, b) for a, b in zip(T.contents(p), T.moved(want, pairs)))
+        assert pool.lens.tolist() == [20, 33, 20, 33, 33, 0]
+
+
 @pytest.mark.parametrize("seed", range(3))
 def test_reserve_of_any_state(seed):
     """Random tables with holes, lengths and counts, with starts and without."""
