@@ -1,6 +1,7 @@
 // Shared by the kernels of the 8-bit paged cache (tq_pages_*.hip).
 #pragma once
 #include "tq_internal.h"
+#include "tq_pages_plan.h"
 
 namespace tq {
 
@@ -104,18 +105,13 @@ struct PagesAttendArgs {
   float* part;  // what they leave, [n_rows][query heads][splits][4 + d]; with one range unused
   Divide by_splits, by_tiles, by_heads, by_new, by_group, by_queries;  // (tiles of rows: of the kernel that is taken; query heads)
 };
-// workgroups of one range each: sequences (or rows) times heads times tiles of query rows
-int64_t pages_attend_units(const BatchView& b, int heads, int group, bool chosen, int tiles);
-struct PagesAttendPlan {
-  bool prompt;
-  int splits, tiles;
-};
-PagesAttendPlan pages_attend_plan(int d, bool f32, const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int64_t window);
+inline PagesAttendSizes pages_attend_sizes(const BatchView& b, int heads, int group, bool chosen, int n_chosen, int log2_page, int window) {
+  return PagesAttendSizes{b.n_seqs, b.max_new, b.width, heads, group, chosen, n_chosen, log2_page, window};
+}
 size_t pages_attend_part_bytes(int d, const BatchView& b, int heads, int group, int splits);
 hipError_t launch_pages_attend(int d, int type, bool f32, const PagesAttendArgs& a, hipStream_t s);
 // many rows of bf16 queries (tq_pages_attend_prompt.hip)
 hipError_t launch_pages_attend_prompt(int d, int type, const PagesAttendArgs& a, hipStream_t s);
-constexpr int pages_prompt_rows(int d) { return d == 256 ? 128 : 256; }  // to a workgroup
 
 // The launches below return hipErrorInvalidConfiguration, and have launched nothing, where a grid does not fit.
 hipError_t launch_pages_append(int d, int type, bool f32, const PagesView& c, const BatchView& b, const PagesRows& k, const PagesRows& v,

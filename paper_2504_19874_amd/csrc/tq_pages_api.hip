@@ -87,7 +87,8 @@ bool attend_fits(const tq_batch* b, int heads, int group, bool chosen) {
 }
 size_t attend_part_bytes(const tq_pages* c, const tq_batch* b, bool f32, int group, bool chosen, int n_chosen, int window, PagesAttendPlan* plan) {
   const BatchView v = view(b);
-  const PagesAttendPlan n = pages_attend_plan(c->d, f32, v, c->n_heads, group, chosen, n_chosen, log2_of(c->page_tokens), window > 0 ? window : INT_MAX);
+  const PagesAttendPlan n = pages_attend_plan(
+      c->d, f32, pages_attend_sizes(v, c->n_heads, group, chosen, n_chosen, log2_of(c->page_tokens), window > 0 ? window : INT_MAX), device_cu_count());
   if (plan != nullptr) *plan = n;
   return pages_attend_part_bytes(c->d, v, c->n_heads, group, n.splits);
 }
