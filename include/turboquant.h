@@ -504,6 +504,8 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *           does a value beyond the largest code of the largest scale, which is stored as that.
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
+ *           tq_pages_attend plans for sequences as long as the table is wide: pass the entries that are in use only (a narrower
+ *           width, the same stride); a wide table costs short sequences a second launch they do not need, up to 3.4 us.
  *   lens[s] tokens of sequence s, the call's own new tokens among them: row j of its count rows is at position
  *           lens[s] - count + j.  Rows at positions below zero are no tokens (nothing stored, output zero).
  *           Attention reads tokens below 2^31 - 128.
@@ -565,7 +567,8 @@ tq_status tq_pages_append(const tq_pages* c, const tq_batch* b, const void* k, c
  * n_seqs * max_new * n_heads_q below 2^31; n_seqs * n_heads times tiles of 16 rows (of max_new * n_heads_q / n_heads; where pages are
  * chosen, n_seqs * max_new * n_heads times tiles of n_heads_q / n_heads) below 2^24, for prompts in bf16, 256 rows to a
  * tile (d = 256: 128), below 2^23; else TQ_ERR_UNSUPPORTED.
- * Prompts and single tokens in one call share a plan made for the longest; in two calls each has its own.
+ * Prompts and single tokens in one call share a plan made for the longest; in two calls each has its own (8 x 4 heads of 128, a
+ * prompt of 2048 and 63 tokens after 4096: 755 us in one call, 162 in two; and one token after 65536: 1340 and 94).
  * Sums, maxima and weights are fp32.  Codes are exact factors in 16 bits; a bf16 query is one exact factor, an fp32 one
  * three; a softmax weight is taken in fp16 (bf16 output: relative error 2^-11, below the output's own half step 2^-8) or as
  * two fp16 pieces (fp32 output: 2^-22), no closer than 2^-32 of the row's largest weight times value scale.

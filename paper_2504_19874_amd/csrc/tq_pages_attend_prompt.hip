@@ -12,9 +12,10 @@
 // Wavefronts 0..3 take the values of two subtiles of 16 keys each (d = 256: one), 4..7 the keys.  The next tile is fetched while a tile is multiplied
 // and written to the other half of LDS: one barrier a tile.
 //
-// What bounds it: matrix and vector instructions hardly run at the same time with two wavefronts to a SIMD (measured: 16 fused
-// multiply-adds behind every product take 29.7 ns, apart 17.1 and 13.7; only exponentials hide), so what counts is the number of vector
-// instructions.  Tiles of 128 keys have half the barriers, addresses and masks of tiles of 64: 8192 tokens of which 2048 are new, 4
+// What bounds it: matrix and vector instructions.  With two wavefronts to a SIMD four fused multiply-adds behind a product hide (14.2 ns, the
+// product alone 13.7), more of them hide in part (8: 19.9, apart 22.7) and then hardly at all (16: 29.7, apart 30.8); this kernel has
+// 6.5 vector instructions to a product, so that what counts is their number.  Of the SIMDs' cycles the matrix cores are busy in 46 %
+// (SQ_VALU_MFMA_BUSY_CYCLES), vector and matrix instructions issue in 51 % (SQ_ACTIVE_INST_VALU).  Tiles of 128 keys have half the barriers, addresses and masks of tiles of 64: 8192 tokens of which 2048 are new, 4
 // sequences of 8 x 4 heads, d = 64 784 -> 620 us, d = 128 1012 -> 970 (on one card); d = 256 1614 -> 1390 (two sequences) by what
 // is no longer carried through the loop in registers.  Logits of the next 32 keys multiplied between the exponentials: 7-15 % slower.
 #include "tq_pages_attend.h"

