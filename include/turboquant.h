@@ -505,7 +505,7 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *   Tables  table[s][i] is the page that holds tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s.  An entry
  *           outside [0, n_pages) is no page: tokens that lie there are not stored, and are not there to be read.
  *           tq_pages_attend plans for sequences as long as the table is wide: pass the entries that are in use only (a narrower
- *           width, the same stride); a wide table costs short sequences a second launch they do not need, up to 3.4 us.
+ *           width, the same stride); a wide table costs short sequences a second launch they do not need, up to 4 us.
  *   lens[s] tokens of sequence s, the call's own new tokens among them: row j of its count rows is at position
  *           lens[s] - count + j.  Rows at positions below zero are no tokens (nothing stored, output zero).
  *           Attention reads tokens below 2^31 - 128.
