@@ -508,7 +508,7 @@ tq_status tq_append(const tq_params* p, const void* x, int32_t dtype, int64_t n,
  *           width, the same stride); a wide table costs short sequences a second launch they do not need, up to 4 us.
  *   lens[s] tokens of sequence s, the call's own new tokens among them: row j of its count rows is at position
  *           lens[s] - count + j.  Rows at positions below zero are no tokens (nothing stored, output zero).
- *           Attention reads tokens below 2^31 - 128.
+ *           Attention reads tokens below 2^31 - 128; a row from there on counts as one at the last of them.
  */
 typedef enum { TQ_PAGE_E4M3 = 0, TQ_PAGE_I8 = 1 } tq_page_type;
 

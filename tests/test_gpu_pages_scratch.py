@@ -201,3 +201,58 @@ def test_reserved_calls_ask_torch_for_nothing(readers):
         assert same(r.results(), want[0]) and p.c.workspace == p.workspace.data_ptr() and p.c.workspace_bytes == p.workspace.numel()
     finally:
         r.p = kept
+
+
+def test_without_the_compiled_half(readers, cache, monkeypatch):
+    from paper_2504_19874_amd import _lib
+    monkeypatch.setattr(_lib, "_call", _lib._Checked())
+    test_streams_of_one_thread(readers)
+    test_threads(readers, False)
+    test_threads(readers, True)
+    test_graphs_that_run_at_once(readers)
+    test_a_stream_that_is_captured_after_eager_calls_on_it(readers)
+    test_sizes_that_creep_up(cache)
+
+
+def test_the_pools_calls_captured():
+    """Fork, free, reserve and compact in a graph: every replay against the same calls made eagerly, from states that differ."""
+    rng = np.random.default_rng(103)
+    heads, page, n_pages, rows, width = 1, 16, 300, 24, 8
+
+    def state():
+        p = tq.make_pages(n_pages, heads, 64, page, dtype=torch.int8, bounds=True, device=DEV)
+        return p, torch.full((rows, width), -1, dtype=torch.int32, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV), ints([0, 0, 0])
+
+    parents, children, ended, starts = ints(np.zeros(8)), ints(np.zeros(8)), ints(np.zeros(5)), ints(np.zeros(rows + 1))
+
+    def call(p, table, lens, told):
+        tq.tq_pages_fork(p, table, lens, parents, children, missing=told[:1])
+        tq.tq_pages_free(p, table, lens, ended)
+        tq.tq_pages_compact(p, table, n_live=told[1:2])
+        lens.add_(starts.diff())
+        tq.tq_pages_reserve(p, table, lens, 20, missing=told[2:], starts=starts)
+
+    a, b = state(), state()
+    call(*state())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*a)
+    for t, u in zip((a[0].k, a[0].v, a[0].k_scale, a[0].bounds), (b[0].k, b[0].v, b[0].k_scale, b[0].bounds)):
+        x = torch.from_numpy(rng.integers(-100, 100, t.shape)).to(t.dtype)
+        t.copy_(x), u.copy_(x)
+    live = 0
+    for i in range(12):
+        new = rng.integers(0, 21, rows)
+        starts.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum(new)])))
+        parents.copy_(torch.from_numpy(rng.integers(0, rows, 8)))
+        children.copy_(torch.from_numpy(rng.integers(0, rows, 8)))
+        ended.copy_(torch.from_numpy(rng.integers(0, rows, 5)))
+        graph.replay()
+        call(*b)
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+        for x, y in zip((*a[1:], a[0].refs, a[0].k, a[0].v, a[0].k_scale, a[0].bounds), (*b[1:], b[0].refs, b[0].k, b[0].v, b[0].k_scale, b[0].bounds)):
+            assert torch.equal(x, y), i
+        live = max(live, int(a[3][1]))
+    assert live > 20
