@@ -100,7 +100,7 @@ class Pages:
 
     def reserve_bytes(self, need: int):
         """Make the calling thread's scratch memory on the current stream at least `need` bytes, so that no call there asks torch for more.
-        Calls of the C ABI with this object's struct (`c`) have it as their workspace; what an earlier one had stays theirs."""
+        It is also the workspace of this object's struct (`c`), for calls of the C ABI; one that it takes the place of there is kept."""
         if need > 0:
             with torch.cuda.device(self.device):
                 c, space = self._with_scratch(need)
